@@ -277,6 +277,101 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
                           const int32_t* n_new, int32_t batch, int32_t num_kv_heads,
                           int32_t max_budget, void* hip_stream);
 
+/* ---- Trees of drafted tokens ------------------------------------------
+ *
+ * A draft that branches proposes a tree: several continuations are verified at
+ * once and the longest accepted path is kept.  The nodes are the last
+ * tree_sizes[b] tokens of a request (append, then attend: seq_lens[b] counts
+ * them, node i is token seq_lens[b] - tree_sizes[b] + i).
+ *
+ * pillar_verify_tree: attention of every node.
+ *   max_nodes  N, 1..64: slots per request in q, visible, out and lse.
+ *   tree_sizes device [B], 0 <= tree_sizes[b] <= N, or NULL: N each.
+ *   q          [B][N][Hq][D] q_dtype; node i is the i-th slot.
+ *   visible    device [B][N] uint64: bit j of visible[b][i] says whether node i
+ *              attends to node j (normally its ancestors and itself; any set of
+ *              nodes will do, and bits from tree_sizes[b] on are ignored).  Every
+ *              node attends to all tokens before the tree.  A chain is
+ *              visible[b][i] = 2^(i+1) - 1, plain decoding N = 1 and a word of 1.
+ *   out, lse, scores, score_stride: as in pillar_verify_attn, the statistic being
+ *              the mean over the tree_sizes[b]*G rows.  Slots from tree_sizes[b]
+ *              on and scores from seq_lens[b] on are not written, nor is anything
+ *              of a request without nodes.  A node that sees no token gets out = 0
+ *              and lse = -inf and adds nothing to the statistic.  What a node does
+ *              not see has no influence on it, whatever the cache holds there
+ *              (infinities and NaN included).
+ * Every shape that pillar_kv_t can describe, page sizes of 1 on, group sizes up
+ * to 16, with up to 1024 rows per KV head.  bf16 queries with a bf16 or fp8 cache
+ * run on bf16 matrix instructions (P is rounded to bf16), if q, out, the pools and
+ * their strides are multiples of 16 bytes; everything else, and with
+ * PILLAR_FLAG_GENERIC_KERNELS everything, on fp32 ones.  lse and scores carry
+ * fp32 rounding only.  PILLAR_FLAG_EXACT_SCORES changes nothing here.
+ * workspace: pillar_tree_workspace_bytes() (0: invalid arguments), enough for any
+ * smaller batch, max_seq_len and N too.
+ *
+ * pillar_tree_commit: the accepted path becomes the end of the context.
+ *   path       device [B][max_path] int32 (max_path 1..64), path_lens device [B]:
+ *              with first = seq_lens[b] - tree_sizes[b], the K and V rows of tokens
+ *              first + path[b][i], i < path_lens[b], move to tokens first + i, all
+ *              read before any is written: nodes may be named in any order, and
+ *              more than once.  A path ends at the first entry outside
+ *              0..tree_sizes[b]-1; a request whose tree is not all in the cache
+ *              (first < 0) commits nothing.
+ *   scores     the statistic of the verification, or NULL: its entries move along.
+ *   new_lens   device [B] int32, receives first + the length of the path; no part of
+ *              it may be kv->seq_lens.
+ * WRITES into the pools and, for fp8, into k_scale and v_scale: a page that
+ * receives rows gets the largest scale that any of its rows up to the new length
+ * had, and those rows are rounded anew to codes of that scale (at most half a
+ * step of e4m3; where the scales are equal the bytes stay).  No page may belong to
+ * two requests.  Pools and strides in multiples of 16 bytes, else
+ * PILLAR_EUNSUPPORTED. */
+size_t pillar_tree_workspace_bytes(const pillar_kv_t* kv, int32_t max_nodes);
+int pillar_verify_tree(const pillar_kv_t* kv, const void* q, int32_t max_nodes,
+                       const int32_t* tree_sizes, const uint64_t* visible,
+                       void* out, float* lse, float* scores, int64_t score_stride,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t max_nodes,
+                       const int32_t* path, const int32_t* path_lens, int32_t max_path,
+                       int32_t* new_lens, float* scores, int64_t score_stride, void* hip_stream);
+
+/* ---- A cache that holds no more than a budget --------------------------
+ *
+ * pillar_evict_kv accumulates the statistic of every verification into a weight
+ * per (request, KV head, cached token) and evicts the tokens that the budget does
+ * not hold; each KV head keeps a set of its own.  For request b, with
+ * L = seq_lens[b] and o = old_lens[b] (tokens the last call left, 0 at first;
+ * those from o on are new):
+ *   weights    device [B][Hkv][state_stride] fp32, in and out:
+ *              w[t] <- decay * w[t] + scores[t] for t < o, scores[t] for o <= t < L.
+ *              scores NULL: the weights of old tokens stay, new ones get 0.
+ *   positions  device [B][Hkv][state_stride] int32, in and out: the place of each
+ *              cached token in the text.  New tokens are numbered on from the
+ *              largest of the old ones (from 0 where there is none).
+ *   budgets    device [B]: K' = min(budgets[b], L) tokens of each head stay:
+ *              first those with a position below sink_tokens or among the
+ *              recent_tokens largest numbers, then those of largest weight;
+ *              whatever is equal is resolved towards the lower slot.  (Weights are
+ *              >= 0; one that is negative or NaN counts as 0.)
+ *   new_lens   device [B] int32, receives K'.  May be kv->seq_lens, old_lens or
+ *              budgets itself, but must not overlap them in part.
+ * Attention does not depend on the order of the rows, so the tokens that stay are
+ * not closed up: those in slots below K' stay where they are and those beyond move
+ * into the freed slots below K', the i-th into the i-th, K, V, weight and position
+ * together.  Pages from ceil(K'/page_size) on are free afterwards; weights and
+ * positions from K' on are left as they were.
+ * WRITES into the pools and, for fp8, into k_scale and v_scale as
+ * pillar_tree_commit does.  No page may belong to two requests.
+ * state_stride >= max_seq_len; 0 <= decay < 1e30; pools and strides in multiples
+ * of 16 bytes, else PILLAR_EUNSUPPORTED.  (Rows leave their order: queries of
+ * a later verification must follow the cached tokens, as they do when appended.)
+ * workspace: pillar_evict_workspace_bytes() (0: invalid description). */
+size_t pillar_evict_workspace_bytes(const pillar_kv_t* kv);
+int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_stride, float decay,
+                    const int32_t* old_lens, const int32_t* budgets, int32_t sink_tokens,
+                    int32_t recent_tokens, float* weights, int32_t* positions, int64_t state_stride,
+                    int32_t* new_lens, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,8 @@ DTYPE_CODE = {"f32": PILLAR_F32, "bf16": PILLAR_BF16, "fp8_e4m3": PILLAR_FP8_E4M
 
 EXPORTS = ("pillar_version", "pillar_status_string", "pillar_workspace_bytes", "pillar_verify_attn",
            "pillar_verify_select", "pillar_verify_hetero", "pillar_mixed_step", "pillar_select_topk", "pillar_sparse_decode", "pillar_sparse_decode_static", "pillar_window_indices",
-           "pillar_extend_indices", "pillar_append_kv", "pillar_profile_enable", "pillar_profile_reset",
+           "pillar_extend_indices", "pillar_append_kv", "pillar_tree_workspace_bytes", "pillar_verify_tree", "pillar_tree_commit",
+           "pillar_evict_workspace_bytes", "pillar_evict_kv", "pillar_profile_enable", "pillar_profile_reset",
            "pillar_profile_read", "pillar_set_option", "pillar_bench_read")
 
 
@@ -103,6 +104,19 @@ def load() -> C.CDLL:
     lib.pillar_extend_indices.restype = C.c_int
     lib.pillar_extend_indices.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                           C.c_void_p]
+    lib.pillar_tree_workspace_bytes.restype = C.c_size_t
+    lib.pillar_tree_workspace_bytes.argtypes = [C.POINTER(pillar_kv_t), C.c_int32]
+    lib.pillar_verify_tree.restype = C.c_int
+    lib.pillar_verify_tree.argtypes = [C.POINTER(pillar_kv_t), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.pillar_tree_commit.restype = C.c_int
+    lib.pillar_tree_commit.argtypes = [C.POINTER(pillar_kv_t), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                       C.c_void_p, C.c_int64, C.c_void_p]
+    lib.pillar_evict_workspace_bytes.restype = C.c_size_t
+    lib.pillar_evict_workspace_bytes.argtypes = [C.POINTER(pillar_kv_t)]
+    lib.pillar_evict_kv.restype = C.c_int
+    lib.pillar_evict_kv.argtypes = [C.POINTER(pillar_kv_t), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                    C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.pillar_bench_read.restype = C.c_int
     lib.pillar_bench_read.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
     lib.pillar_set_option.restype = C.c_int
@@ -275,6 +289,83 @@ def pillar_extend_indices(indices: torch.Tensor, counts: torch.Tensor, first_new
     rc = load().pillar_extend_indices(indices.data_ptr(), counts.data_ptr(), first_new.data_ptr(), n_new.data_ptr(),
                                       indices.shape[0], indices.shape[1], indices.shape[2], _stream(stream))
     _check(rc, "pillar_extend_indices")
+
+
+# ---- trees of drafted tokens, a bounded cache ----
+_Q_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _tensor(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
+    """The address of a tensor whose type, shape and layout are what the C side takes for granted."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}"
+                         f"{'' if t.is_contiguous() else ', strided'}")
+    return t.data_ptr()
+
+
+def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, B: int, Hkv: int, max_seq_len: int, what: str) -> tuple:
+    """Address and stride of [B][Hkv][stride]: rows of at least max_seq_len entries, one behind the other."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.dim() != 3 or t.shape[0] != B or t.shape[1] != Hkv or t.shape[2] < max_seq_len or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor [{B}, {Hkv}, >= {max_seq_len}] is wanted, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), t.shape[2]
+
+
+def pillar_tree_workspace_bytes(kv: KvCache, max_nodes: int) -> int:
+    s = kv.c_struct()
+    return int(load().pillar_tree_workspace_bytes(C.byref(s), max_nodes))
+
+
+def pillar_verify_tree(kv: KvCache, q: torch.Tensor, tree_sizes: Optional[torch.Tensor], visible: torch.Tensor, out: torch.Tensor,
+                       lse: Optional[torch.Tensor], scores: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """visible: int64 [B, N], the bit patterns of the 64-bit words."""
+    s = kv.c_struct()
+    B, N = visible.shape
+    shape = (B, N, s.num_q_heads, s.head_dim)
+    if B != s.batch:
+        raise ValueError(f"visible: a row for each of {s.batch} requests is wanted, not {B}")
+    scores_at, stride = _rows(scores, torch.float32, B, s.num_kv_heads, s.max_seq_len, "scores")
+    rc = load().pillar_verify_tree(C.byref(s), _tensor(q, _Q_TORCH[kv.q_dtype], shape, "q"), N, _tensor(tree_sizes, torch.int32, (B,), "tree_sizes"),
+                                   _tensor(visible, torch.int64, (B, N), "visible"), _tensor(out, _Q_TORCH[kv.q_dtype], shape, "out"),
+                                   _tensor(lse, torch.float32, shape[:3], "lse"), scores_at, stride, workspace.data_ptr(),
+                                   workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(rc, "pillar_verify_tree")
+
+
+def pillar_tree_commit(kv: KvCache, tree_sizes: Optional[torch.Tensor], max_nodes: int, path: torch.Tensor, path_lens: torch.Tensor,
+                       new_lens: torch.Tensor, scores: Optional[torch.Tensor] = None, stream=None) -> None:
+    s = kv.c_struct()
+    B, M = s.batch, path.shape[-1]
+    scores_at, stride = _rows(scores, torch.float32, B, s.num_kv_heads, s.max_seq_len, "scores")
+    rc = load().pillar_tree_commit(C.byref(s), _tensor(tree_sizes, torch.int32, (B,), "tree_sizes"), max_nodes,
+                                   _tensor(path, torch.int32, (B, M), "path"), _tensor(path_lens, torch.int32, (B,), "path_lens"), M,
+                                   _tensor(new_lens, torch.int32, (B,), "new_lens"), scores_at, stride, _stream(stream))
+    _check(rc, "pillar_tree_commit")
+
+
+def pillar_evict_workspace_bytes(kv: KvCache) -> int:
+    s = kv.c_struct()
+    return int(load().pillar_evict_workspace_bytes(C.byref(s)))
+
+
+def pillar_evict_kv(kv: KvCache, scores: Optional[torch.Tensor], decay: float, old_lens: torch.Tensor, budgets: torch.Tensor,
+                    sink_tokens: int, recent_tokens: int, weights: torch.Tensor, positions: torch.Tensor, new_lens: torch.Tensor,
+                    workspace: torch.Tensor, stream=None) -> None:
+    s = kv.c_struct()
+    B, Hkv, top = s.batch, s.num_kv_heads, s.max_seq_len
+    scores_at, stride = _rows(scores, torch.float32, B, Hkv, top, "scores")
+    weights_at, state_stride = _rows(weights, torch.float32, B, Hkv, top, "weights")
+    positions_at, other = _rows(positions, torch.int32, B, Hkv, top, "positions")
+    if other != state_stride:
+        raise ValueError("weights and positions: rows of one length are wanted")
+    rc = load().pillar_evict_kv(C.byref(s), scores_at, stride, decay, _tensor(old_lens, torch.int32, (B,), "old_lens"),
+                                _tensor(budgets, torch.int32, (B,), "budgets"), sink_tokens, recent_tokens, weights_at, positions_at,
+                                state_stride, _tensor(new_lens, torch.int32, (B,), "new_lens"), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(rc, "pillar_evict_kv")
 
 
 def pillar_bench_read(buf: torch.Tensor, n_chunks: int, chunk_bytes: int, order: Optional[torch.Tensor], blocks: int,

@@ -75,6 +75,49 @@ struct TopkArgs {
   int32_t* counts;
 };
 
+struct TreeArgs {
+  KvView kv;
+  const void* q;
+  const int32_t* tree_sizes;   // null: max_nodes each
+  const uint64_t* visible;
+  int32_t max_nodes;
+  void* out;
+  float* lse;                  // may be null
+  float* scores;               // may be null
+  int64_t score_stride;
+  int32_t q_dtype, kv_dtype;
+  bool generic;                // PILLAR_FLAG_GENERIC_KERNELS: fp32 arithmetic whatever the types
+  void* workspace;
+};
+
+struct CommitArgs {
+  KvView kv;
+  const int32_t* tree_sizes;   // null: max_nodes each
+  int32_t max_nodes, max_path;
+  const int32_t* path;
+  const int32_t* path_lens;
+  int32_t* new_lens;
+  float* scores;               // may be null
+  int64_t score_stride;
+  int32_t kv_dtype;
+};
+
+struct EvictArgs {
+  KvView kv;
+  const float* scores;         // may be null
+  int64_t score_stride;
+  float decay;
+  const int32_t* old_lens;
+  const int32_t* budgets;
+  int32_t sink_tokens, recent_tokens;
+  float* weights;
+  int32_t* positions;
+  int64_t state_stride;
+  int32_t* new_lens;
+  int32_t kv_dtype;
+  void* workspace;
+};
+
 // generic (any supported shape, fp32 arithmetic)
 // fine_room: what small launches make use of; without it, the least the kernels run with
 size_t verify_generic_workspace(const KvView& kv, int n_q, bool fine_room);
@@ -103,6 +146,17 @@ DecWs decode_carve(const KvView& kv, int max_budget, void* workspace);
 hipError_t launch_decode_merge(const DecodeArgs& a, hipStream_t s);          // combines the spans of lists longer than one
 size_t decode_static_scratch_bytes();                     // size of the library's own scratch array
 hipError_t launch_decode_mfma_static(const DecodeArgs& a, hipStream_t s);   // same kernels, partials in that array
+
+// trees of drafted tokens (verify_tree.hip, tree_commit.hip)
+int tree_nodes_max();
+bool verify_tree_counts(const KvView& kv, int max_nodes);                    // the units of work can be counted in 32 bits
+size_t verify_tree_workspace(const KvView& kv, int max_nodes);
+hipError_t launch_verify_tree(const TreeArgs& a, hipStream_t s);
+hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t s);
+
+// eviction by accumulated weight (evict.hip)
+size_t evict_workspace(const KvView& kv);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 
 // process-wide tuning knobs (pillar_set_option); 0 = default
 struct Options {

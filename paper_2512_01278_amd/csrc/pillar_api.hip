@@ -125,6 +125,22 @@ int check_workspace(const void* ws, size_t have, size_t need) {
   return PILLAR_OK;
 }
 
+// rows are copied in 16-byte pieces: pools and strides are multiples of that
+bool rows_in_pieces(const pillar_kv_t* kv) {
+  const int64_t esz = kv->kv_dtype == PILLAR_F32 ? 4 : kv->kv_dtype == PILLAR_BF16 ? 2 : 1;
+  return (kv->stride_page * esz) % 16 == 0 && (kv->stride_head * esz) % 16 == 0 && (kv->stride_slot * esz) % 16 == 0 &&
+         ((reinterpret_cast<uintptr_t>(kv->k_pool) | reinterpret_cast<uintptr_t>(kv->v_pool)) & 15u) == 0;
+}
+
+// requests and heads are the second and third dimension of a grid
+bool fits_a_grid(const pillar_kv_t* kv) { return kv->batch <= 65535 && kv->num_kv_heads <= 65535; }
+
+int check_nodes(const pillar_kv_t* kv, int max_nodes) {
+  if (max_nodes < 1) return PILLAR_EINVAL;
+  if (max_nodes > tree_nodes_max() || !fits_a_grid(kv)) return PILLAR_EUNSUPPORTED;
+  return PILLAR_OK;
+}
+
 // The size that is reported has room for the generic kernels' fine chunks; without it (a size that a build before those chunks
 // reported), calls run all the same.
 size_t verify_workspace(const KvView& v, int n_q, bool fine_room) {
@@ -474,6 +490,102 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
   if (batch < 1 || num_kv_heads < 1 || max_budget < 1) return PILLAR_EINVAL;
   return launch_extend_indices(indices, counts, first_new, n_new, batch, num_kv_heads, max_budget,
                                static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+size_t pillar_tree_workspace_bytes(const pillar_kv_t* kv, int32_t max_nodes) {
+  if (check_kv(kv) != PILLAR_OK || check_nodes(kv, max_nodes) != PILLAR_OK) return 0;
+  const KvView v = make_view(kv);
+  return verify_tree_counts(v, max_nodes) ? verify_tree_workspace(v, max_nodes) : 0;
+}
+
+int pillar_verify_tree(const pillar_kv_t* kv, const void* q, int32_t max_nodes, const int32_t* tree_sizes, const uint64_t* visible,
+                       void* out, float* lse, float* scores, int64_t score_stride, void* workspace, size_t workspace_bytes,
+                       void* hip_stream) {
+  int rc = check_kv(kv);
+  if (rc != PILLAR_OK) return rc;
+  rc = check_nodes(kv, max_nodes);
+  if (rc != PILLAR_OK) return rc;
+  if (!q || !visible || !out) return PILLAR_EINVAL;
+  if (scores && score_stride < kv->max_seq_len) return PILLAR_EINVAL;
+  TreeArgs a;
+  a.kv = make_view(kv);
+  if (!verify_tree_counts(a.kv, max_nodes)) return PILLAR_EUNSUPPORTED;
+  rc = check_workspace(workspace, workspace_bytes, verify_tree_workspace(a.kv, max_nodes));
+  if (rc != PILLAR_OK) return rc;
+  a.q = q;
+  a.tree_sizes = tree_sizes;
+  a.visible = visible;
+  a.max_nodes = max_nodes;
+  a.out = out;
+  a.lse = lse;
+  a.scores = scores;
+  a.score_stride = score_stride;
+  a.q_dtype = kv->q_dtype;
+  a.kv_dtype = kv->kv_dtype;
+  a.generic = (kv->flags & PILLAR_FLAG_GENERIC_KERNELS) != 0;
+  a.workspace = workspace;
+  return launch_verify_tree(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t max_nodes, const int32_t* path, const int32_t* path_lens,
+                       int32_t max_path, int32_t* new_lens, float* scores, int64_t score_stride, void* hip_stream) {
+  int rc = check_kv(kv);
+  if (rc != PILLAR_OK) return rc;
+  rc = check_nodes(kv, max_nodes);
+  if (rc != PILLAR_OK) return rc;
+  if (!path || !path_lens || !new_lens || max_path < 1) return PILLAR_EINVAL;
+  if (max_path > tree_nodes_max()) return PILLAR_EUNSUPPORTED;
+  if (scores && score_stride < kv->max_seq_len) return PILLAR_EINVAL;
+  // the heads of a request read its length while one of them writes the new one
+  const uintptr_t lens = reinterpret_cast<uintptr_t>(kv->seq_lens), now = reinterpret_cast<uintptr_t>(new_lens), span = static_cast<uintptr_t>(kv->batch) * 4;
+  if (now < lens + span && lens < now + span) return PILLAR_EINVAL;
+  if (!rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
+  CommitArgs a;
+  a.kv = make_view(kv);
+  a.tree_sizes = tree_sizes;
+  a.max_nodes = max_nodes;
+  a.max_path = max_path;
+  a.path = path;
+  a.path_lens = path_lens;
+  a.new_lens = new_lens;
+  a.scores = scores;
+  a.score_stride = score_stride;
+  a.kv_dtype = kv->kv_dtype;
+  return launch_tree_commit(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+size_t pillar_evict_workspace_bytes(const pillar_kv_t* kv) {
+  if (check_kv(kv) != PILLAR_OK || !fits_a_grid(kv)) return 0;
+  return evict_workspace(make_view(kv));
+}
+
+int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_stride, float decay, const int32_t* old_lens,
+                    const int32_t* budgets, int32_t sink_tokens, int32_t recent_tokens, float* weights, int32_t* positions,
+                    int64_t state_stride, int32_t* new_lens, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_kv(kv);
+  if (rc != PILLAR_OK) return rc;
+  if (!old_lens || !budgets || !weights || !positions || !new_lens) return PILLAR_EINVAL;
+  if (!(decay >= 0.f) || !(decay < 1e30f) || sink_tokens < 0 || recent_tokens < 0) return PILLAR_EINVAL;
+  if (state_stride < kv->max_seq_len || (scores && score_stride < kv->max_seq_len)) return PILLAR_EINVAL;
+  if (!fits_a_grid(kv) || !rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
+  EvictArgs a;
+  a.kv = make_view(kv);
+  rc = check_workspace(workspace, workspace_bytes, evict_workspace(a.kv));
+  if (rc != PILLAR_OK) return rc;
+  a.scores = scores;
+  a.score_stride = score_stride;
+  a.decay = decay;
+  a.old_lens = old_lens;
+  a.budgets = budgets;
+  a.sink_tokens = sink_tokens;
+  a.recent_tokens = recent_tokens;
+  a.weights = weights;
+  a.positions = positions;
+  a.state_stride = state_stride;
+  a.new_lens = new_lens;
+  a.kv_dtype = kv->kv_dtype;
+  a.workspace = workspace;
+  return launch_evict(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
 }
 
 int pillar_set_option(const char* name, int64_t value) {

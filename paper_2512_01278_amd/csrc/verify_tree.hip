@@ -1,0 +1,721 @@
+// Verification of a tree of drafted tokens over the paged cache.
+//
+// Paper Section 4.1 verifies a chain: query i sees everything up to its own position.  Here the n drafted tokens, the last n of
+// the context, form a tree (or any graph): node i sees the tokens before the tree and those nodes whose bit its word has.
+//
+//   out  = softmax(sm_scale q K^T over what the node sees) V
+//   lse  = log sum exp of the same logits
+//   scores[t] = 1 / (n G) sum over the rows of exp(sm_scale q k_t - lse)          (the statistic; optional)
+//
+// Launches:
+//   tree_pass    one pass over K and V with the running maximum and sum of every row's softmax.  A unit of work is TS tokens of one (request, KV
+//                head, tile of RT rows); all units in a row are cut into equal ranges, one per resident workgroup, so lengths on the
+//                device need no plan on the host.  A stretch of one tile that a range does not hold whole leaves a partial (m, l, O).
+//   tree_merge   joins the partials.
+//   tree_scores  (with scores) K once more against the final log-sum-exp, summed over the rows.  With n G rows a stash of P would be 2 n G
+//                bytes a token written and read where K's second read is 2 D: at 64 and more rows the read is less.
+#include <algorithm>
+
+#include "host_rules.hpp"
+#include "launch.hpp"
+#include "tree_tile.hpp"
+
+namespace pillar {
+namespace {
+
+constexpr int kTreeNodes = 64;
+
+struct TreeParams {
+  KvView kv;
+  const void* q;
+  const int32_t* tree_sizes;   // null: max_nodes each
+  const uint64_t* visible;
+  void* out;
+  float* lse;                  // may be null
+  int32_t max_nodes, group, q_dtype;
+  bool aligned;                // cache rows can be read 16 bytes at a time
+  // workspace
+  int32_t* prefix;             // [B+1] units before a request, and all of them
+  float* part_ml;              // [slots][RT][2]
+  float* part_o;               // [slots][RT][D]
+  float* lse2;                 // [B][max_nodes][Hq], in log2 units; only with scores
+  int32_t ranges;              // workgroups of the pass
+};
+
+// Units are counted the same way by the pass and the merge.
+struct Shape {
+  int len, nodes, rows, steps, tiles;
+};
+template <int TS, int RT>
+__device__ __forceinline__ Shape shape_of(const TreeParams& a, int b) {
+  Shape s;
+  s.len = min(max(a.kv.seq_lens[b], 0), a.kv.max_seq_len);
+  s.nodes = a.tree_sizes ? min(max(a.tree_sizes[b], 0), a.max_nodes) : a.max_nodes;
+  s.rows = s.nodes * a.group;
+  s.steps = (s.len + TS - 1) / TS;
+  s.tiles = (s.rows + RT - 1) / RT;
+  return s;
+}
+template <int TS, int RT>
+__device__ __forceinline__ int units_of(const TreeParams& a, int b) {
+  const Shape s = shape_of<TS, RT>(a, b);
+  return s.steps * s.tiles * a.kv.num_kv_heads;
+}
+
+// Range w of n has units range_begin(w) .. range_begin(w + 1) - 1.
+struct Ranges {
+  int n, each, longer;         // the first `longer` ranges have each + 1 units, the others `each`
+  __device__ __forceinline__ Ranges(int total, int workgroups) {
+    n = max(1, min(total, workgroups));
+    each = total / n;
+    longer = total - each * n;
+  }
+  __device__ __forceinline__ int begin(int w) const { return w * each + min(w, longer); }
+  __device__ __forceinline__ int of(int u) const {          // the range that has unit u
+    const int split = longer * (each + 1);
+    return u < split ? u / (each + 1) : longer + (u - split) / each;
+  }
+};
+
+__device__ __forceinline__ int wave_inclusive(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(v, o, 64);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+
+template <int D_, int KV_, bool F32, int WR_, int WT_, int NS_>
+struct Cfg {
+  static constexpr int D = D_, KV = KV_, WR = WR_, WT = WT_, NS = NS_;     // WR x WT wavefronts: groups of 32 rows x groups of tokens
+  using E = std::conditional_t<F32, EngineF32<D>, EngineBf16<D>>;
+  static constexpr int kWaves = WR * WT, kThreads = 64 * kWaves;
+  static constexpr int kGroupTokens = 32 * NS, TS = kGroupTokens * WT, RT = 32 * WR;
+  static constexpr int kPieces = D * kv_bytes<KV>() / 16;                  // 16-byte pieces of a row
+  static constexpr int kLoads = (TS * kPieces + kThreads - 1) / kThreads;  // of K, and as many of V, per thread and tile
+  static constexpr bool kAllLoad = TS * kPieces >= kThreads;
+  static constexpr bool kScales = KV == PILLAR_FP8_E4M3 && !F32;           // page scales are applied to logits and P
+  static constexpr int kTileBytes = TS * (E::kKPitch + E::kVPitch);
+  static constexpr int kJoinRow = D + 4;                                   // floats
+  static constexpr int kJoinBytes = WT > 1 ? kWaves * 32 * kJoinRow * 4 : 0;
+  static constexpr int kLds = kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes;
+};
+
+// The rows of a tile that a thread carries, between global memory and LDS.
+template <typename C>
+struct Carrier {
+  using E = typename C::E;
+  int64_t base;                // elements: this head's rows in page 0
+  const int32_t* table;
+  int last;                    // the last token: rows past it are read there
+  int pid[C::kLoads];
+  u32x4 k[C::kLoads], v[C::kLoads];
+  int scale_pid;
+  float ks, vs;
+
+  static __device__ __forceinline__ int row(int u) { return (threadIdx.x + u * C::kThreads) / C::kPieces; }
+  static __device__ __forceinline__ int piece(int u) { return (threadIdx.x + u * C::kThreads) % C::kPieces; }
+  static __device__ __forceinline__ bool carries() { return C::kAllLoad || threadIdx.x < C::TS * C::kPieces; }
+
+  __device__ __forceinline__ int token(int step, int r) const { return min(step * C::TS + r, last); }
+  __device__ __forceinline__ void pages(const KvView& kv, int step) {
+#pragma unroll
+    for (int u = 0; u < C::kLoads; ++u) pid[u] = carries() ? table[token(step, row(u)) >> kv.page_shift] : 0;
+    if (C::kScales) scale_pid = table[token(step, min<int>(threadIdx.x, C::TS - 1)) >> kv.page_shift];
+  }
+  __device__ __forceinline__ int64_t elem(const KvView& kv, int step, int u) const {
+    return base + static_cast<int64_t>(pid[u]) * kv.stride_page + static_cast<int64_t>(token(step, row(u)) & (kv.page_size - 1)) * kv.stride_slot +
+           piece(u) * (16 / kv_bytes<C::KV>());
+  }
+  __device__ __forceinline__ void fetch(const KvView& kv, int g, int step) {
+    if (carries()) {
+#pragma unroll
+      for (int u = 0; u < C::kLoads; ++u) {
+        const int64_t at = elem(kv, step, u);
+        k[u] = load_piece<C::KV>(kv.k_pool, at, true);
+        v[u] = load_piece<C::KV>(kv.v_pool, at, true);
+      }
+    }
+    if (C::kScales) {
+      const int64_t at = static_cast<int64_t>(scale_pid) * kv.num_kv_heads + g;
+      ks = kv.k_scale[at];
+      vs = kv.v_scale[at];
+    }
+  }
+};
+
+template <typename C>
+__global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(TreeParams a) {
+  using E = typename C::E;
+  constexpr int D = C::D, TS = C::TS, RT = C::RT;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[C::kLds];
+  __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? TS : 4], s_vs[C::kScales ? TS : 4];
+  __shared__ float s_m[C::kWaves][32], s_l[C::kWaves][32];
+  __shared__ uint32_t s_bad[2][TS / 32];
+  const KvView& kv = a.kv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % C::WR, wt = wave / C::WR;
+  const int n = lane & 31, g2 = lane >> 5;
+  uint8_t* const ktile = smem;
+  uint8_t* const vtile = smem + TS * E::kKPitch;
+  const float scale2 = kv.sm_scale * kLog2e;
+
+  // ---- the plan, by every wavefront ----
+  int total = 0;
+  for (int c = 0; c < kv.batch; c += 64) {
+    const int b = c + lane;
+    total += __shfl(wave_inclusive(b < kv.batch ? units_of<TS, RT>(a, b) : 0, lane), 63, 64);
+  }
+  const Ranges ranges(total, a.ranges);
+  // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
+  int w = blockIdx.x;
+  if (ranges.n == a.ranges && a.ranges % 8 == 0) w = (w & 7) * (a.ranges >> 3) + (w >> 3);
+  if (w >= ranges.n) return;
+  const bool leader = w == 0 && wave == 0;               // leaves the prefix for the merge
+  const int u0 = ranges.begin(w), u1 = ranges.begin(w + 1);
+  int b = 0, ub = 0;           // the request at work and its first unit
+  {
+    int before = 0;
+    bool found = false;
+    for (int c = 0; c < kv.batch; c += 64) {
+      const int r = c + lane;
+      const int mine = r < kv.batch ? units_of<TS, RT>(a, r) : 0;
+      const int upto = wave_inclusive(mine, lane) + before;
+      if (leader && r < kv.batch) a.prefix[r] = upto - mine;
+      if (!found) {
+        const uint64_t after = __ballot(upto > u0);
+        if (after) {
+          const int at = __builtin_ctzll(after);
+          b = c + at;
+          ub = __shfl(upto - mine, at, 64);
+          found = true;
+        }
+      }
+      before = __shfl(upto, 63, 64);
+      if (found && !leader) break;
+    }
+    if (leader && lane == 0) a.prefix[kv.batch] = total;
+  }
+  if (total == 0) return;
+  if (tid < TS / 32) s_bad[0][tid] = 0;
+  int parity = 0;              // of the tile: the other half of s_bad is cleared meanwhile
+  __syncthreads();
+
+  for (int u = u0; u < u1;) {
+    b = __builtin_amdgcn_readfirstlane(b);
+    const Shape sh = shape_of<TS, RT>(a, b);
+    const int units = sh.steps * sh.tiles * kv.num_kv_heads;
+    if (u >= ub + units) {     // (a request without units among them)
+      ub += units;
+      ++b;
+      continue;
+    }
+    const int rel = u - ub, pair = rel / sh.steps, s0 = rel - pair * sh.steps;
+    const int g = pair / sh.tiles, tile = pair - g * sh.tiles;
+    const int s1 = min(sh.steps, s0 + (u1 - u));
+    const bool whole = s0 == 0 && s1 == sh.steps;
+    const int slot = 2 * w + (u == u0 ? 0 : 1);
+    u += s1 - s0;
+
+    // ---- rows ----
+    const int row = tile * RT + wr * 32 + n;             // of the (request, head)'s nodes x group
+    const bool there = row < sh.rows, any_row = tile * RT + wr * 32 < sh.rows;
+    const int node = there ? row / a.group : 0, head = g * a.group + (there ? row - node * a.group : 0);
+    const int64_t out_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + head;
+    typename E::Query qf;
+    E::load_query(qf, a.q, out_row, there, a.q_dtype, g2);
+    const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
+    const int first_node = sh.len - sh.nodes;            // token of node 0 (below 0: it is not in the cache)
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    Carrier<C> c;
+    c.base = static_cast<int64_t>(g) * kv.stride_head;
+    c.table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
+    c.last = sh.len - 1;
+    if constexpr (!E::kF32) {
+      c.pages(kv, s0);
+      c.fetch(kv, g, s0);
+      if (s0 + 1 < s1) c.pages(kv, s0 + 1);
+    }
+
+    for (int s = s0; s < s1; ++s, parity ^= 1) {
+      const bool tail = (s + 1) * TS > first_node;       // some token of the tile is a node, or past the end
+      // ---- the tile into LDS ----
+      if constexpr (!E::kF32) {
+        if (c.carries()) {
+#pragma unroll
+          for (int i = 0; i < C::kLoads; ++i) {
+            const int r = c.row(i);
+            park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + r * E::kKPitch, c.piece(i));
+            if (!tail) {
+              park_piece<E, C::KV, false>(c.v[i], 1.f, vtile + r * E::kVPitch, c.piece(i));
+            } else if (park_piece<E, C::KV, true>(c.v[i], 1.f, vtile + r * E::kVPitch, c.piece(i))) {
+              atomicOr(&s_bad[parity][r >> 5], 1u << (r & 31));
+            }
+          }
+        }
+        if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
+      } else {
+#pragma unroll 4
+        for (int i = 0; i < C::kLoads; ++i) {
+          const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
+          if (c.carries()) {
+            const int64_t at = c.base + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
+                               c.piece(i) * (16 / kv_bytes<C::KV>());
+            const u32x4 kx = load_piece<C::KV>(kv.k_pool, at, a.aligned), vx = load_piece<C::KV>(kv.v_pool, at, a.aligned);
+            float ks = 1.f, vs = 1.f;
+            if constexpr (C::KV == PILLAR_FP8_E4M3) {
+              ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
+              vs = kv.v_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
+            }
+            park_piece<E, C::KV, false>(kx, ks, ktile + r * E::kKPitch, c.piece(i));
+            if (!tail) {
+              park_piece<E, C::KV, false>(vx, vs, vtile + r * E::kVPitch, c.piece(i));
+            } else if (park_piece<E, C::KV, true>(vx, vs, vtile + r * E::kVPitch, c.piece(i))) {
+              atomicOr(&s_bad[parity][r >> 5], 1u << (r & 31));
+            }
+          }
+        }
+      }
+      __syncthreads();
+      if constexpr (!E::kF32) {
+        if (s + 1 < s1) {
+          c.fetch(kv, g, s + 1);
+          if (s + 2 < s1) c.pages(kv, s + 2);
+        }
+      }
+      if (tid < TS / 32) s_bad[parity ^ 1][tid] = 0;
+
+      // ---- 32 tokens at a time ----
+      if (any_row) {
+#pragma unroll
+        for (int sub = 0; sub < C::NS; ++sub) {
+          const int at = wt * C::kGroupTokens + 32 * sub, t0 = s * TS + at;
+          if (t0 >= sh.len) break;
+          const bool masked = t0 + 32 > first_node;
+          f32x16 x = E::qk(ktile + at * E::kKPitch, qf, lane);
+          if constexpr (C::kScales) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const f32x4 f = *reinterpret_cast<const f32x4*>(s_ks + at + elem_of(i, g2));
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[i + j] *= f[j];
+            }
+          }
+          uint32_t sees = 0xffffu;                       // bit i: this row sees the token of element i
+          if (masked) {
+            sees = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int j = t0 + elem_of(i, g2) - first_node;
+              const bool vis = j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1));
+              sees |= static_cast<uint32_t>(vis) << i;
+              x[i] = vis ? x[i] : -INFINITY;
+            }
+          }
+          float top = x[0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+          top = other_half_max(top) * scale2;
+          // The maximum that exponentials are relative to moves only when a logit exceeds it by more than 8 (in log2 units): P stays below
+          // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.
+          if (__any(top > m_run + 8.f)) {
+            const float m_new = fmaxf(m_run, top);
+            const float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
+            m_run = m_new;
+            l_run *= f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[db][i] *= f;
+          }
+          const float m_use = m_run == -INFINITY ? 0.f : m_run;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] = fast_exp2(__builtin_fmaf(x[i], scale2, -m_use));
+            sum += x[i];
+          }
+          l_run += sum;
+          const uint32_t bad = masked ? __builtin_amdgcn_readfirstlane(s_bad[parity][at >> 5]) : 0;
+          if (bad) {
+            // What is not finite in V counts for the rows that see its token only: it was left out of the tile, and is added here.
+            for (uint32_t left = bad; left; left &= left - 1) {
+              const int tok = __builtin_ctz(left), src = (tok >> 3) * 4 + (tok & 3);
+              float p = 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) p = i == src ? x[i] : p;
+              p = __shfl(p, n + 32 * ((tok >> 2) & 1), 64);
+              const bool vis = __shfl(static_cast<int>(sees >> src & 1u), n + 32 * ((tok >> 2) & 1), 64) != 0;
+              const int t = t0 + tok;
+              if (t >= sh.len) continue;
+              int page;
+              const int64_t e0 = row_offset(kv, b, g, t, &page);
+              float vs = 1.f;
+              if constexpr (C::KV == PILLAR_FP8_E4M3) vs = kv.v_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
+#pragma unroll
+              for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  float val = Storage<C::KV>::load(kv.v_pool, e0 + 32 * db + elem_of(i, g2)) * vs;
+                  const float kept = val;
+                  if (drop_nonfinite(val) && vis) o[db][i] += p * kept;
+                  __builtin_amdgcn_sched_barrier(0);     // one at a time: the path is never taken, and costs no registers so
+                }
+            }
+          }
+          if constexpr (C::kScales) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const f32x4 f = *reinterpret_cast<const f32x4*>(s_vs + at + elem_of(i, g2));
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[i + j] *= f[j];
+            }
+            if (masked) {                                // (the scale of a page that no row sees may be anything)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = (sees >> i & 1u) ? x[i] : 0.f;
+            }
+          }
+          E::pv(vtile + at * E::kVPitch, x, o, lane);
+        }
+      }
+      __syncthreads();
+    }
+
+    // ---- what the stretch leaves ----
+    l_run = other_half_sum(l_run);
+    const int tile_row = wr * 32 + n;
+    auto leave_row = [&](int64_t to_row, int in_tile, float m, float l) {        // one lane per row
+      if (whole) {
+        const float y = l == 0.f ? -INFINITY : m + log2f(l);
+        if (a.lse) a.lse[to_row] = y * kLn2;
+        if (a.lse2) a.lse2[to_row] = y;
+      } else {
+        float* ml = a.part_ml + (static_cast<int64_t>(slot) * RT + in_tile) * 2;
+        ml[0] = m;
+        ml[1] = l;
+      }
+    };
+    auto leave_dims = [&](int64_t to_row, int in_tile, int dim, f32x4 x, float inv) {
+      if (!whole) {
+        *reinterpret_cast<f32x4*>(a.part_o + (static_cast<int64_t>(slot) * RT + in_tile) * D + dim) = x;
+      } else if (!E::kF32) {
+        u32x2 y;
+        y.x = f32_to_bf16(x[0] * inv) | static_cast<uint32_t>(f32_to_bf16(x[1] * inv)) << 16;
+        y.y = f32_to_bf16(x[2] * inv) | static_cast<uint32_t>(f32_to_bf16(x[3] * inv)) << 16;
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_row * D + dim) = y;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to_row * D + dim + j, x[j] * inv);
+          else Storage<PILLAR_BF16>::store(a.out, to_row * D + dim + j, x[j] * inv);
+        }
+      }
+    };
+    if constexpr (C::WT == 1) {
+      if (there) {
+        if (g2 == 0) leave_row(out_row, tile_row, m_run, l_run);
+        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            leave_dims(out_row, tile_row, 32 * db + elem_of(i, g2), f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]}, inv);
+      }
+    } else {
+      // the wavefronts that shared the rows join in LDS, where the tile was
+      float* join = reinterpret_cast<float*>(smem);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(join + (wave * 32 + n) * C::kJoinRow + 32 * db + elem_of(i, g2)) = f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
+      if (g2 == 0) { s_m[wave][n] = m_run; s_l[wave][n] = l_run; }
+      __syncthreads();
+      constexpr int kQuads = D / 4;
+      for (int e = tid; e < RT * kQuads; e += C::kThreads) {
+        const int r = e / kQuads, dim = 4 * (e % kQuads), rr = tile * RT + r;
+        if (rr >= sh.rows) continue;
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < C::WT; ++k) m = fmaxf(m, s_m[k * C::WR + (r >> 5)][r & 31]);
+        const float m_use = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        f32x4 x = {};
+#pragma unroll
+        for (int k = 0; k < C::WT; ++k) {
+          const int from = k * C::WR + (r >> 5);
+          const float f = fast_exp2(s_m[from][r & 31] - m_use);
+          l += s_l[from][r & 31] * f;
+          x += *reinterpret_cast<const f32x4*>(join + (from * 32 + (r & 31)) * C::kJoinRow + dim) * f;
+        }
+        const int nd = rr / a.group;
+        const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + nd) * kv.num_q_heads + g * a.group + (rr - nd * a.group);
+        if (dim == 0) leave_row(to, r, m, l);
+        leave_dims(to, r, dim, x, l == 0.f ? 0.f : 1.f / l);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---- joins what several ranges left of a tile: 32 rows per workgroup, a row to D/4 lanes ----
+template <int D, int TS, int RT>
+__global__ __launch_bounds__(256) void tree_merge(TreeParams a, int tiles_max) {
+  constexpr int kQuads = D / 4, kRows = 256 / kQuads;
+  const KvView& kv = a.kv;
+  const int b = blockIdx.y, g = blockIdx.x / tiles_max, tile = blockIdx.x % tiles_max;
+  const Shape sh = shape_of<TS, RT>(a, b);
+  const int row_end = min(sh.rows, tile * RT + RT), row0 = tile * RT + blockIdx.z * 32;
+  if (row0 >= row_end) return;
+  int w0 = 0, w1 = -1, first = 0;
+  if (sh.steps > 0) {
+    const Ranges ranges(a.prefix[kv.batch], a.ranges);
+    first = a.prefix[b] + (g * sh.tiles + tile) * sh.steps;
+    w0 = ranges.of(first);
+    w1 = ranges.of(first + sh.steps - 1);
+    if (w0 == w1) return;                                // the pass wrote the final values
+    first = 2 * w0 + (ranges.begin(w0) < first ? 1 : 0); // slot of the first stretch; the others begin their range
+  }
+  const int dim = 4 * (threadIdx.x % kQuads);
+  for (int row = row0 + threadIdx.x / kQuads; row < min(row_end, row0 + 32); row += kRows) {
+    const int r = row - tile * RT;
+    auto ml_of = [&](int w) { return a.part_ml + (static_cast<int64_t>(w == w0 ? first : 2 * w) * RT + r) * 2; };
+    float m = -INFINITY;
+    for (int w = w0; w <= w1; ++w) m = fmaxf(m, ml_of(w)[0]);
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 x = {};
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+      const float* ml = ml_of(w);
+      const float f = fast_exp2(ml[0] - m_use);
+      l += ml[1] * f;
+      x += *reinterpret_cast<const f32x4*>(a.part_o + (static_cast<int64_t>(w == w0 ? first : 2 * w) * RT + r) * D + dim) * f;
+    }
+    const int node = row / a.group;
+    const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
+    if (dim == 0) {
+      const float y = l == 0.f ? -INFINITY : m + log2f(l);
+      if (a.lse) a.lse[to] = y * kLn2;
+      if (a.lse2) a.lse2[to] = y;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to * D + dim + j, x[j] * inv);
+      else Storage<PILLAR_BF16>::store(a.out, to * D + dim + j, x[j] * inv);
+    }
+  }
+}
+
+// ---- the statistic: a workgroup has 128 tokens of a (request, KV head), 32 to a wavefront, whose K rows wait in registers; the rows
+// pass by in tiles of 32 through LDS ----
+template <int D, int KV, bool F32>
+__global__ __launch_bounds__(256) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
+  using E = std::conditional_t<F32, EngineF32<D>, EngineBf16<D>>;
+  constexpr int kPieces = D * kv_bytes<KV>() / 16;
+  __shared__ __attribute__((aligned(16))) uint8_t s_k[128 * E::kKPitch];
+  __shared__ float s_ks[128];
+  __shared__ float s_sum[128];
+  const KvView& kv = a.kv;
+  const int b = blockIdx.z, g = blockIdx.y, t_begin = blockIdx.x * 128;
+  const Shape sh = shape_of<128, 32>(a, b);
+  if (t_begin >= sh.len || sh.rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g2 = lane >> 5;
+  const float scale2 = kv.sm_scale * kLog2e;
+  const int first_node = sh.len - sh.nodes;
+#pragma unroll 4
+  for (int e = tid; e < 128 * kPieces; e += 256) {
+    const int r = e / kPieces, piece = e % kPieces;
+    int page;
+    const int64_t at = row_offset(kv, b, g, min(t_begin + r, sh.len - 1), &page) + piece * (16 / kv_bytes<KV>());
+    float ks = 1.f;
+    if constexpr (KV == PILLAR_FP8_E4M3) ks = kv.k_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
+    if (piece == 0) s_ks[r] = F32 ? 1.f : ks;
+    park_piece<E, KV, false>(load_piece<KV>(kv.k_pool, at, a.aligned), ks, s_k + r * E::kKPitch, piece);
+  }
+  __syncthreads();
+  const int at = wave * 32, t0 = t_begin + at;
+  float sum[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  if (t0 < sh.len) {
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = s_ks[at + elem_of(i, g2)] * scale2;
+    const bool masked = t0 + 32 > first_node;
+    for (int r0 = 0; r0 < sh.rows; r0 += 32) {
+      const int row = r0 + n;
+      const bool there = row < sh.rows;
+      const int node = there ? row / a.group : 0;
+      const int64_t q_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (there ? row - node * a.group : 0);
+      typename E::Query qf;
+      E::load_query(qf, a.q, q_row, there, a.q_dtype, g2);
+      float y = there ? a.lse2[q_row] : INFINITY;
+      if (y == -INFINITY) y = INFINITY;                  // a row that sees nothing has no share
+      const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
+      const f32x16 x = E::qk(s_k + at * E::kKPitch, qf, lane);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float p = fast_exp2(__builtin_fmaf(x[i], f[i], -y));
+        if (masked) {
+          const int j = t0 + elem_of(i, g2) - first_node;
+          p = (j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1))) && there ? p : 0.f;
+        }
+        sum[i] += there ? p : 0.f;
+      }
+    }
+  }
+  // over the 32 rows of a half wavefront
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor(sum[i], o, 64);
+    if (n == 0) s_sum[at + elem_of(i, g2)] = sum[i];
+  }
+  __syncthreads();
+  float* out = scores + (static_cast<int64_t>(b) * kv.num_kv_heads + g) * score_stride;
+  if (tid < 128 && t_begin + tid < sh.len) out[t_begin + tid] = s_sum[tid] / static_cast<float>(sh.rows);
+}
+
+// ------------------------------------------------------------------ host --
+struct TreePlan {
+  int rt, ts, ranges, tiles_max;
+  int64_t slots;
+};
+
+// Wavefronts side by side on the rows: as many groups of 32 as there are rows, up to 8; the others of a workgroup of four take other tokens.
+TreePlan plan_of(const KvView& kv, int max_nodes, bool f32) {
+  TreePlan p;
+  const int rows = max_nodes * (kv.num_q_heads / kv.num_kv_heads);
+  const int groups = (rows + 31) / 32;
+  int per_cu;
+  if (f32) {
+    p.rt = groups <= 1 ? 32 : 128;
+    p.ts = groups <= 1 ? 128 : 64;
+    per_cu = 1;
+  } else {
+    p.rt = groups <= 1 ? 32 : groups <= 2 ? 64 : groups <= 4 ? 128 : 256;
+    p.ts = groups <= 1 ? 128 : 64;
+    per_cu = groups <= 4 ? 2 : 1;
+  }
+  p.tiles_max = (rows + p.rt - 1) / p.rt;
+  const int64_t most = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * p.tiles_max * ((kv.max_seq_len + p.ts - 1) / p.ts);
+  p.ranges = static_cast<int>(std::min<int64_t>(most, static_cast<int64_t>(per_cu) * num_cus()));
+  p.slots = 2 * static_cast<int64_t>(p.ranges);
+  return p;
+}
+
+struct TreeWs {
+  size_t ml, o, lse2, bytes;
+};
+TreeWs carve(const KvView& kv, int max_nodes, const TreePlan& p) {
+  TreeWs w;
+  size_t at = align_up((static_cast<size_t>(kv.batch) + 1) * 4, 256);
+  w.ml = at;
+  at = align_up(at + static_cast<size_t>(p.slots) * p.rt * 8, 256);
+  w.o = at;
+  at = align_up(at + static_cast<size_t>(p.slots) * p.rt * kv.head_dim * 4, 256);
+  w.lse2 = at;
+  at = align_up(at + static_cast<size_t>(kv.batch) * max_nodes * kv.num_q_heads * 4, 256);
+  w.bytes = at;
+  return w;
+}
+
+bool rows_aligned(const KvView& kv, int kv_dtype) {
+  const int64_t per = kv_dtype == PILLAR_F32 ? 4 : kv_dtype == PILLAR_BF16 ? 8 : 16;       // elements per 16 bytes
+  return kv.stride_page % per == 0 && kv.stride_head % per == 0 && kv.stride_slot % per == 0 &&
+         ((reinterpret_cast<uintptr_t>(kv.k_pool) | reinterpret_cast<uintptr_t>(kv.v_pool)) & 15u) == 0;
+}
+
+template <typename C>
+hipError_t launch_tree(const TreeParams& p, const TreePlan& plan, const TreeArgs& t, hipStream_t s) {
+  static_assert(C::kLds + 2 * C::TS * 4 + 64 * C::kWaves * 4 + 64 <= 160 * 1024, "");
+  {
+    KernelTimer timer("tree_pass", s);
+    hipLaunchKernelGGL((tree_pass<C>), dim3(p.ranges), dim3(C::kThreads), 0, s, p);
+  }
+  {
+    KernelTimer timer("tree_merge", s);
+    hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT>), dim3(p.kv.num_kv_heads * plan.tiles_max, p.kv.batch, C::RT / 32), dim3(256), 0, s, p,
+                       plan.tiles_max);
+  }
+  if (t.scores) {
+    KernelTimer timer("tree_scores", s);
+    hipLaunchKernelGGL((tree_scores<C::D, C::KV, C::E::kF32>), dim3((p.kv.max_seq_len + 127) / 128, p.kv.num_kv_heads, p.kv.batch), dim3(256), 0, s, p, t.scores,
+                       t.score_stride);
+  }
+  return hipGetLastError();
+}
+
+template <int D, int KV>
+hipError_t launch_bf16(const TreeParams& p, const TreePlan& plan, const TreeArgs& t, hipStream_t s) {
+  switch (plan.rt) {
+    case 32: return launch_tree<Cfg<D, KV, false, 1, 4, 1>>(p, plan, t, s);
+    case 64: return launch_tree<Cfg<D, KV, false, 2, 2, 1>>(p, plan, t, s);
+    case 128: return launch_tree<Cfg<D, KV, false, 4, 1, 2>>(p, plan, t, s);
+    default: return launch_tree<Cfg<D, KV, false, 8, 1, 2>>(p, plan, t, s);
+  }
+}
+template <int D, int KV>
+hipError_t launch_f32(const TreeParams& p, const TreePlan& plan, const TreeArgs& t, hipStream_t s) {
+  if (plan.rt == 32) return launch_tree<Cfg<D, KV, true, 1, 4, 1>>(p, plan, t, s);
+  return launch_tree<Cfg<D, KV, true, 4, 1, 2>>(p, plan, t, s);
+}
+
+}  // namespace
+
+int tree_nodes_max() { return kTreeNodes; }
+
+// The workspace has room for either engine: which one runs depends on the alignment of the tensors of a call.
+size_t verify_tree_workspace(const KvView& kv, int max_nodes) {
+  return std::max(carve(kv, max_nodes, plan_of(kv, max_nodes, false)).bytes, carve(kv, max_nodes, plan_of(kv, max_nodes, true)).bytes);
+}
+
+// units are counted in 32 bits
+bool verify_tree_counts(const KvView& kv, int max_nodes) {
+  const int64_t tiles = (static_cast<int64_t>(max_nodes) * (kv.num_q_heads / kv.num_kv_heads) + 31) / 32;
+  return static_cast<int64_t>(kv.batch) * kv.num_kv_heads * tiles * ((static_cast<int64_t>(kv.max_seq_len) + 63) / 64) < (int64_t{1} << 30) && kv.batch <= 65535;
+}
+
+hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
+  const KvView& kv = t.kv;
+  const bool f32 = t.generic || t.q_dtype != PILLAR_BF16 || t.kv_dtype == PILLAR_F32 || !rows_aligned(kv, t.kv_dtype) ||
+                   ((reinterpret_cast<uintptr_t>(t.q) | reinterpret_cast<uintptr_t>(t.out)) & 15u) != 0;
+  const TreePlan plan = plan_of(kv, t.max_nodes, f32);
+  const TreeWs w = carve(kv, t.max_nodes, plan);
+  char* ws = static_cast<char*>(t.workspace);
+  TreeParams p;
+  p.kv = kv;
+  p.q = t.q;
+  p.tree_sizes = t.tree_sizes;
+  p.visible = t.visible;
+  p.out = t.out;
+  p.lse = t.lse;
+  p.max_nodes = t.max_nodes;
+  p.group = kv.num_q_heads / kv.num_kv_heads;
+  p.q_dtype = t.q_dtype;
+  p.aligned = rows_aligned(kv, t.kv_dtype);
+  p.prefix = reinterpret_cast<int32_t*>(ws);
+  p.part_ml = reinterpret_cast<float*>(ws + w.ml);
+  p.part_o = reinterpret_cast<float*>(ws + w.o);
+  p.lse2 = t.scores ? reinterpret_cast<float*>(ws + w.lse2) : nullptr;
+  p.ranges = plan.ranges;
+  const bool wide = kv.head_dim == 128;
+  if (!f32) {
+    if (t.kv_dtype == PILLAR_BF16) return wide ? launch_bf16<128, PILLAR_BF16>(p, plan, t, s) : launch_bf16<64, PILLAR_BF16>(p, plan, t, s);
+    return wide ? launch_bf16<128, PILLAR_FP8_E4M3>(p, plan, t, s) : launch_bf16<64, PILLAR_FP8_E4M3>(p, plan, t, s);
+  }
+  switch (t.kv_dtype) {
+    case PILLAR_F32: return wide ? launch_f32<128, PILLAR_F32>(p, plan, t, s) : launch_f32<64, PILLAR_F32>(p, plan, t, s);
+    case PILLAR_BF16: return wide ? launch_f32<128, PILLAR_BF16>(p, plan, t, s) : launch_f32<64, PILLAR_BF16>(p, plan, t, s);
+    default: return wide ? launch_f32<128, PILLAR_FP8_E4M3>(p, plan, t, s) : launch_f32<64, PILLAR_FP8_E4M3>(p, plan, t, s);
+  }
+}
+
+}  // namespace pillar
