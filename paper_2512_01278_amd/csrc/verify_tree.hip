@@ -102,6 +102,19 @@ struct Cfg {
   static constexpr int kLds = kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes;
 };
 
+// Results of the rows of a request that has nothing to see, by a whole workgroup.
+template <int D>
+__device__ __forceinline__ void see_nothing(const TreeParams& a, int b, int nodes) {
+  const int64_t first = static_cast<int64_t>(b) * a.max_nodes * a.kv.num_q_heads;
+  const int rows = nodes * a.kv.num_q_heads;
+  for (int e = threadIdx.x; e < rows * D; e += blockDim.x) {
+    if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, first * D + e, 0.f);
+    else Storage<PILLAR_BF16>::store(a.out, first * D + e, 0.f);
+  }
+  if (a.lse)
+    for (int r = threadIdx.x; r < rows; r += blockDim.x) a.lse[first + r] = -INFINITY;
+}
+
 // The rows of a tile that a thread carries, between global memory and LDS.
 template <typename C>
 struct Carrier {
@@ -152,7 +165,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   __shared__ __attribute__((aligned(16))) uint8_t smem[C::kLds];
   __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? TS : 4], s_vs[C::kScales ? TS : 4];
   __shared__ float s_m[C::kWaves][32], s_l[C::kWaves][32];
-  __shared__ uint32_t s_bad[2][TS / 32];
+  __shared__ uint32_t s_bad[2][2];                       // nodes whose V row is not finite throughout
   const KvView& kv = a.kv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % C::WR, wt = wave / C::WR;
@@ -164,8 +177,15 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   // ---- the plan, by every wavefront ----
   int total = 0;
   for (int c = 0; c < kv.batch; c += 64) {
-    const int b = c + lane;
-    total += __shfl(wave_inclusive(b < kv.batch ? units_of<TS, RT>(a, b) : 0, lane), 63, 64);
+    const int r = c + lane;
+    Shape sh = {};
+    if (r < kv.batch) sh = shape_of<TS, RT>(a, r);
+    total += __shfl(wave_inclusive(sh.steps * sh.tiles * kv.num_kv_heads, lane), 63, 64);
+    // contexts without a token have no unit: their rows are shared out among the workgroups
+    for (uint64_t none = __ballot(sh.len == 0 && sh.nodes > 0); none; none &= none - 1) {
+      const int at = __builtin_ctzll(none);
+      if ((c + at) % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) see_nothing<D>(a, c + at, __shfl(sh.nodes, at, 64));
+    }
   }
   const Ranges ranges(total, a.ranges);
   // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
@@ -198,8 +218,8 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     if (leader && lane == 0) a.prefix[kv.batch] = total;
   }
   if (total == 0) return;
-  if (tid < TS / 32) s_bad[0][tid] = 0;
-  int parity = 0;              // of the tile: the other half of s_bad is cleared meanwhile
+  if (tid < 2) s_bad[0][tid] = 0;
+  int parity = 0;              // of the stretch: the other half of s_bad is cleared meanwhile
   __syncthreads();
 
   for (int u = u0; u < u1;) {
@@ -242,7 +262,18 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
       if (s0 + 1 < s1) c.pages(kv, s0 + 1);
     }
 
-    for (int s = s0; s < s1; ++s, parity ^= 1) {
+    // What is not finite in a node's V counts for the rows that see the node only: it is left out of the tile, and added at the end.
+    auto park_v = [&](const u32x4& x, float scale, int s, int r, int piece, bool tail) {
+      uint8_t* to = vtile + r * E::kVPitch;
+      const int t = s * TS + r;
+      if (!tail || t < first_node) {
+        park_piece<E, C::KV, false>(x, scale, to, piece);
+      } else if (park_piece<E, C::KV, true>(x, scale, to, piece) && t < sh.len) {
+        atomicOr(&s_bad[parity][(t - first_node) >> 5], 1u << ((t - first_node) & 31));
+      }
+    };
+
+    for (int s = s0; s < s1; ++s) {
       const bool tail = (s + 1) * TS > first_node;       // some token of the tile is a node, or past the end
       // ---- the tile into LDS ----
       if constexpr (!E::kF32) {
@@ -251,11 +282,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
           for (int i = 0; i < C::kLoads; ++i) {
             const int r = c.row(i);
             park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + r * E::kKPitch, c.piece(i));
-            if (!tail) {
-              park_piece<E, C::KV, false>(c.v[i], 1.f, vtile + r * E::kVPitch, c.piece(i));
-            } else if (park_piece<E, C::KV, true>(c.v[i], 1.f, vtile + r * E::kVPitch, c.piece(i))) {
-              atomicOr(&s_bad[parity][r >> 5], 1u << (r & 31));
-            }
+            park_v(c.v[i], 1.f, s, r, c.piece(i), tail);
           }
         }
         if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
@@ -273,11 +300,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
               vs = kv.v_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
             }
             park_piece<E, C::KV, false>(kx, ks, ktile + r * E::kKPitch, c.piece(i));
-            if (!tail) {
-              park_piece<E, C::KV, false>(vx, vs, vtile + r * E::kVPitch, c.piece(i));
-            } else if (park_piece<E, C::KV, true>(vx, vs, vtile + r * E::kVPitch, c.piece(i))) {
-              atomicOr(&s_bad[parity][r >> 5], 1u << (r & 31));
-            }
+            park_v(vx, vs, s, r, c.piece(i), tail);
           }
         }
       }
@@ -288,7 +311,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
           if (s + 2 < s1) c.pages(kv, s + 2);
         }
       }
-      if (tid < TS / 32) s_bad[parity ^ 1][tid] = 0;
+      if (s == s0 && tid < 2) s_bad[parity ^ 1][tid] = 0;
 
       // ---- 32 tokens at a time ----
       if (any_row) {
@@ -306,9 +329,8 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
               for (int j = 0; j < 4; ++j) x[i + j] *= f[j];
             }
           }
-          uint32_t sees = 0xffffu;                       // bit i: this row sees the token of element i
+          uint32_t sees = 0;                             // bit i: this row sees the token of element i
           if (masked) {
-            sees = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int j = t0 + elem_of(i, g2) - first_node;
@@ -341,33 +363,6 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
             sum += x[i];
           }
           l_run += sum;
-          const uint32_t bad = masked ? __builtin_amdgcn_readfirstlane(s_bad[parity][at >> 5]) : 0;
-          if (bad) {
-            // What is not finite in V counts for the rows that see its token only: it was left out of the tile, and is added here.
-            for (uint32_t left = bad; left; left &= left - 1) {
-              const int tok = __builtin_ctz(left), src = (tok >> 3) * 4 + (tok & 3);
-              float p = 0.f;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) p = i == src ? x[i] : p;
-              p = __shfl(p, n + 32 * ((tok >> 2) & 1), 64);
-              const bool vis = __shfl(static_cast<int>(sees >> src & 1u), n + 32 * ((tok >> 2) & 1), 64) != 0;
-              const int t = t0 + tok;
-              if (t >= sh.len) continue;
-              int page;
-              const int64_t e0 = row_offset(kv, b, g, t, &page);
-              float vs = 1.f;
-              if constexpr (C::KV == PILLAR_FP8_E4M3) vs = kv.v_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
-#pragma unroll
-              for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  float val = Storage<C::KV>::load(kv.v_pool, e0 + 32 * db + elem_of(i, g2)) * vs;
-                  const float kept = val;
-                  if (drop_nonfinite(val) && vis) o[db][i] += p * kept;
-                  __builtin_amdgcn_sched_barrier(0);     // one at a time: the path is never taken, and costs no registers so
-                }
-            }
-          }
           if constexpr (C::kScales) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
@@ -385,6 +380,26 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
       }
       __syncthreads();
     }
+
+    const uint64_t bad = __builtin_amdgcn_readfirstlane(s_bad[parity][0]) | static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(s_bad[parity][1])) << 32;
+    for (uint64_t left = bad; left; left &= left - 1) {
+      const int j = __builtin_ctzll(left), t = first_node + j;
+      if ((t % TS) / C::kGroupTokens != wt) continue;    // (the wavefronts whose maximum has seen the token)
+      int page;
+      const int64_t at = row_offset(kv, b, g, t, &page);
+      float vs = 1.f;
+      if constexpr (C::KV == PILLAR_FP8_E4M3) vs = kv.v_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float val = Storage<C::KV>::load(kv.v_pool, at + 32 * db + elem_of(i, g2)) * vs;
+          const float was = val;
+          if (drop_nonfinite(val) && (word >> j & 1)) o[db][i] += was;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    parity ^= 1;
 
     // ---- what the stretch leaves ----
     l_run = other_half_sum(l_run);
@@ -463,129 +478,244 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   }
 }
 
-// ---- joins what several ranges left of a tile: 32 rows per workgroup, a row to D/4 lanes ----
+// ---- joins what several ranges left of a tile.  A tile is cut where a range begins inside it, so there is a row of workgroups for each range, which
+// do nothing unless theirs is the first to begin inside its tile.  A row has D/4 lanes: they fetch (m, l) of as many partials side by
+// side, then the partials of O, eight under way. ----
 template <int D, int TS, int RT>
-__global__ __launch_bounds__(256) void tree_merge(TreeParams a, int tiles_max) {
-  constexpr int kQuads = D / 4, kRows = 256 / kQuads;
+__global__ __launch_bounds__(256) void tree_merge(TreeParams a) {
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
   const KvView& kv = a.kv;
-  const int b = blockIdx.y, g = blockIdx.x / tiles_max, tile = blockIdx.x % tiles_max;
-  const Shape sh = shape_of<TS, RT>(a, b);
-  const int row_end = min(sh.rows, tile * RT + RT), row0 = tile * RT + blockIdx.z * 32;
-  if (row0 >= row_end) return;
-  int w0 = 0, w1 = -1, first = 0;
-  if (sh.steps > 0) {
-    const Ranges ranges(a.prefix[kv.batch], a.ranges);
-    first = a.prefix[b] + (g * sh.tiles + tile) * sh.steps;
-    w0 = ranges.of(first);
-    w1 = ranges.of(first + sh.steps - 1);
-    if (w0 == w1) return;                                // the pass wrote the final values
-    first = 2 * w0 + (ranges.begin(w0) < first ? 1 : 0); // slot of the first stretch; the others begin their range
+  const int lane = threadIdx.x & 63, part = threadIdx.x % kLanes;
+  const Ranges ranges(a.prefix[kv.batch], a.ranges);
+  const int w = blockIdx.x + 1;
+  if (w >= ranges.n) return;
+  const int u = ranges.begin(w);
+  int b = 0;
+  for (int c = 0; c < kv.batch; c += 64) {
+    const uint64_t after = __ballot(c + lane < kv.batch && a.prefix[min(c + lane, kv.batch - 1) + 1] > u);
+    if (after) {
+      b = c + __builtin_ctzll(after);
+      break;
+    }
   }
-  const int dim = 4 * (threadIdx.x % kQuads);
-  for (int row = row0 + threadIdx.x / kQuads; row < min(row_end, row0 + 32); row += kRows) {
-    const int r = row - tile * RT;
-    auto ml_of = [&](int w) { return a.part_ml + (static_cast<int64_t>(w == w0 ? first : 2 * w) * RT + r) * 2; };
-    float m = -INFINITY;
-    for (int w = w0; w <= w1; ++w) m = fmaxf(m, ml_of(w)[0]);
-    const float m_use = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    f32x4 x = {};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const float* ml = ml_of(w);
-      const float f = fast_exp2(ml[0] - m_use);
-      l += ml[1] * f;
-      x += *reinterpret_cast<const f32x4*>(a.part_o + (static_cast<int64_t>(w == w0 ? first : 2 * w) * RT + r) * D + dim) * f;
-    }
-    const int node = row / a.group;
-    const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
-    if (dim == 0) {
-      const float y = l == 0.f ? -INFINITY : m + log2f(l);
-      if (a.lse) a.lse[to] = y * kLn2;
-      if (a.lse2) a.lse2[to] = y;
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+  b = __builtin_amdgcn_readfirstlane(b);
+  const Shape sh = shape_of<TS, RT>(a, b);
+  const int before = a.prefix[b], index = (u - before) / sh.steps, first = before + index * sh.steps;
+  if (first == u) return;                                // the range begins with the tile
+  const int w0 = ranges.of(first), w1 = ranges.of(first + sh.steps - 1);
+  if (w0 != w - 1) return;
+  const int first_slot = 2 * w0 + (ranges.begin(w0) < first ? 1 : 0);      // the others begin their range
+  const int g = index / sh.tiles, tile = index - g * sh.tiles;
+  const int r = blockIdx.y * kRows + threadIdx.x / kLanes, row = tile * RT + r;
+  if (row >= sh.rows) return;
+  const int count = w1 - w0 + 1;
+  auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? first_slot : 2 * (w0 + i)) * RT + r; };
+  float m = -INFINITY;
+  for (int c = 0; c < count; c += kLanes)
+    if (c + part < count) m = fmaxf(m, a.part_ml[2 * at(c + part)]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to * D + dim + j, x[j] * inv);
-      else Storage<PILLAR_BF16>::store(a.out, to * D + dim + j, x[j] * inv);
+  for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kLanes));
+  const float m_use = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  f32x4 x = {};
+  for (int c = 0; c < count; c += kLanes) {
+    float f = 0.f;
+    if (c + part < count) {
+      const float* ml = a.part_ml + 2 * at(c + part);
+      f = fast_exp2(ml[0] - m_use);
+      l += ml[1] * f;
     }
+    const int here = min(kLanes, count - c);
+    for (int i = 0; i < here; i += 8) {
+      f32x4 o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = *reinterpret_cast<const f32x4*>(a.part_o + at(min(c + i + j, count - 1)) * D + 4 * part);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j < here) x += o[j] * __shfl(f, i + j, kLanes);
+    }
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, kLanes);
+  const int node = row / a.group;
+  const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
+  if (part == 0) {
+    const float y = l == 0.f ? -INFINITY : m + log2f(l);
+    if (a.lse) a.lse[to] = y * kLn2;
+    if (a.lse2) a.lse2[to] = y;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to * D + 4 * part + j, x[j] * inv);
+    else Storage<PILLAR_BF16>::store(a.out, to * D + 4 * part + j, x[j] * inv);
   }
 }
 
-// ---- the statistic: a workgroup has 128 tokens of a (request, KV head), 32 to a wavefront, whose K rows wait in registers; the rows
-// pass by in tiles of 32 through LDS ----
-template <int D, int KV, bool F32>
-__global__ __launch_bounds__(256) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
+// ---- the statistic: exp(logit - lse) summed over the rows.  A wavefront keeps the K rows of 64 tokens (32 in fp32) in registers as operands and the
+// query rows pass by, 32 at a time, through LDS, fetched one tile ahead.  64 tokens, as the four wavefronts read each tile of Q whole:
+// 32 KB of LDS reads per 4 x 2 x 32 x 32 x 128 products, half of what the matrix cores take in the time. ----
+template <int D_, int KV_, bool F32>
+struct ScoreCfg {
+  static constexpr int D = D_, KV = KV_;
   using E = std::conditional_t<F32, EngineF32<D>, EngineBf16<D>>;
-  constexpr int kPieces = D * kv_bytes<KV>() / 16;
-  __shared__ __attribute__((aligned(16))) uint8_t s_k[128 * E::kKPitch];
-  __shared__ float s_ks[128];
-  __shared__ float s_sum[128];
+  static constexpr int kSubs = F32 ? 1 : 2, kTokens = 4 * 32 * kSubs;      // tokens of a workgroup
+  static constexpr int kQPieces = D * (F32 ? 4 : 2) / 16;                  // 16-byte pieces of a query row in LDS
+  static constexpr int kQLoads = 32 * kQPieces / 256;
+};
+
+template <typename C>
+__global__ __launch_bounds__(256, 2) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
+  using E = typename C::E;
+  constexpr int D = C::D, KV = C::KV;
+  __shared__ __attribute__((aligned(16))) uint8_t s_q[2][32 * E::kKPitch];
+  __shared__ float s_sum[C::kTokens];
   const KvView& kv = a.kv;
-  const int b = blockIdx.z, g = blockIdx.y, t_begin = blockIdx.x * 128;
-  const Shape sh = shape_of<128, 32>(a, b);
+  const int b = blockIdx.z, g = blockIdx.y, t_begin = blockIdx.x * C::kTokens;
+  const Shape sh = shape_of<C::kTokens, 32>(a, b);
   if (t_begin >= sh.len || sh.rows == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g2 = lane >> 5;
   const float scale2 = kv.sm_scale * kLog2e;
-  const int first_node = sh.len - sh.nodes;
-#pragma unroll 4
-  for (int e = tid; e < 128 * kPieces; e += 256) {
-    const int r = e / kPieces, piece = e % kPieces;
-    int page;
-    const int64_t at = row_offset(kv, b, g, min(t_begin + r, sh.len - 1), &page) + piece * (16 / kv_bytes<KV>());
-    float ks = 1.f;
-    if constexpr (KV == PILLAR_FP8_E4M3) ks = kv.k_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
-    if (piece == 0) s_ks[r] = F32 ? 1.f : ks;
-    park_piece<E, KV, false>(load_piece<KV>(kv.k_pool, at, a.aligned), ks, s_k + r * E::kKPitch, piece);
-  }
-  __syncthreads();
-  const int at = wave * 32, t0 = t_begin + at;
-  float sum[16];
+  const int first_node = sh.len - sh.nodes, t0 = t_begin + wave * 32 * C::kSubs;
+
+  auto row_at = [&](int row) {                           // of q and lse; row < sh.rows
+    const int node = row / a.group;
+    return (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
+  };
+  // ---- a tile of query rows on its way ----
+  u32x4 q_next[C::kQLoads];
+  float y_next;
+  uint64_t word_next;
+  auto fetch = [&](int r0) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  if (t0 < sh.len) {
-    float f[16];
+    for (int u = 0; u < C::kQLoads; ++u) {
+      const int e = tid + 256 * u, row = r0 + e / C::kQPieces, piece = e % C::kQPieces;
+      q_next[u] = u32x4{0, 0, 0, 0};
+      if (row < sh.rows) {
+        const int64_t at = row_at(row) * D;
+        if constexpr (E::kF32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = s_ks[at + elem_of(i, g2)] * scale2;
-    const bool masked = t0 + 32 > first_node;
-    for (int r0 = 0; r0 < sh.rows; r0 += 32) {
-      const int row = r0 + n;
-      const bool there = row < sh.rows;
-      const int node = there ? row / a.group : 0;
-      const int64_t q_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (there ? row - node * a.group : 0);
-      typename E::Query qf;
-      E::load_query(qf, a.q, q_row, there, a.q_dtype, g2);
-      float y = there ? a.lse2[q_row] : INFINITY;
-      if (y == -INFINITY) y = INFINITY;                  // a row that sees nothing has no share
-      const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
-      const f32x16 x = E::qk(s_k + at * E::kKPitch, qf, lane);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float p = fast_exp2(__builtin_fmaf(x[i], f[i], -y));
-        if (masked) {
-          const int j = t0 + elem_of(i, g2) - first_node;
-          p = (j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1))) && there ? p : 0.f;
+          for (int j = 0; j < 4; ++j) {
+            const int64_t i = at + 4 * piece + j;
+            q_next[u][j] = __float_as_uint(a.q_dtype == PILLAR_F32 ? Storage<PILLAR_F32>::load(a.q, i) : Storage<PILLAR_BF16>::load(a.q, i));
+          }
+        } else {
+          q_next[u] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + 8 * piece);
         }
-        sum[i] += there ? p : 0.f;
+      }
+    }
+    const int row = r0 + n;
+    y_next = INFINITY;
+    word_next = 0;
+    if (row < sh.rows) {
+      y_next = a.lse2[row_at(row)];
+      word_next = a.visible[static_cast<int64_t>(b) * a.max_nodes + row / a.group];
+    }
+  };
+  auto park = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < C::kQLoads; ++u) {
+      const int e = tid + 256 * u;
+      *reinterpret_cast<u32x4*>(s_q[buf] + (e / C::kQPieces) * E::kKPitch + 16 * (e % C::kQPieces)) = q_next[u];
+    }
+  };
+  fetch(0);
+
+  // ---- K rows as operands: of 32 tokens, lane (m, g2) has token m, dims 16 s + 8 g2 .. + 7 (fp32: 8 s + 4 g2 .. + 3) ----
+  typename E::Query k[C::kSubs];
+  float f[C::kSubs];                                     // logit scale of this lane's token ...
+#pragma unroll
+  for (int sub = 0; sub < C::kSubs; ++sub) {
+    int page;
+    const int64_t at = row_offset(kv, b, g, min(t0 + 32 * sub + n, sh.len - 1), &page);
+    f[sub] = 1.f;
+    if constexpr (KV == PILLAR_FP8_E4M3) f[sub] = kv.k_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
+    if constexpr (E::kF32) {
+#pragma unroll
+      for (int s = 0; s < D / 8; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          k[sub].q[s][c] = Storage<KV>::load(kv.k_pool, at + 8 * s + 4 * g2 + c);
+          if constexpr (KV == PILLAR_FP8_E4M3) k[sub].q[s][c] *= f[sub];
+        }
+      f[sub] = 1.f;
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        if constexpr (KV == PILLAR_BF16) {
+          k[sub].q[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(kv.k_pool) + at + 16 * s + 8 * g2));
+        } else {
+          const u32x2 c = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(kv.k_pool) + at + 16 * s + 8 * g2);
+          k[sub].q[s] = widen_fp8x8(c.x, c.y);
+        }
       }
     }
   }
+  float sum[C::kSubs][16], scale[C::kSubs][16];          // ... and of the tokens of its accumulator elements
+#pragma unroll
+  for (int sub = 0; sub < C::kSubs; ++sub)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sum[sub][i] = 0.f;
+      scale[sub][i] = KV == PILLAR_FP8_E4M3 ? __shfl(f[sub], elem_of(i, g2), 64) * scale2 : scale2;
+    }
+
+  int buf = 0;
+  for (int r0 = 0; r0 < sh.rows; r0 += 32, buf ^= 1) {
+    park(buf);
+    const float y = y_next == -INFINITY ? INFINITY : y_next;       // a row that sees nothing has no share
+    const uint64_t word = word_next;
+    const bool there = r0 + n < sh.rows;
+    __syncthreads();                                     // (the other buffer is read no more: its readers are past this barrier's predecessor)
+    if (r0 + 32 < sh.rows) fetch(r0 + 32);
+    if (t0 >= sh.len) continue;
+    const uint8_t* q = s_q[buf] + n * E::kKPitch + 16 * g2;
+    f32x16 x[C::kSubs] = {};
+    if constexpr (E::kF32) {
+#pragma unroll
+      for (int s = 0; s < D / 8; ++s) {
+        const f32x4 qv = *reinterpret_cast<const f32x4*>(q + 32 * s);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[0].q[s][c], qv[c], x[0], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(q + 32 * s));
+#pragma unroll
+        for (int sub = 0; sub < C::kSubs; ++sub) x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[sub].q[s], qv, x[sub], 0, 0, 0);
+      }
+    }
+    const bool masked = t0 + 32 * C::kSubs > first_node || r0 + 32 > sh.rows;
+#pragma unroll
+    for (int sub = 0; sub < C::kSubs; ++sub)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float p = fast_exp2(__builtin_fmaf(x[sub][i], scale[sub][i], -y));
+        if (masked) {
+          const int j = t0 + 32 * sub + elem_of(i, g2) - first_node;
+          p = there && (j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1))) ? p : 0.f;
+        }
+        sum[sub][i] += p;
+      }
+  }
   // over the 32 rows of a half wavefront
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int sub = 0; sub < C::kSubs; ++sub)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor(sum[i], o, 64);
-    if (n == 0) s_sum[at + elem_of(i, g2)] = sum[i];
-  }
+    for (int i = 0; i < 16; ++i) {
+      float v = row16_sum(sum[sub][i]);
+      v += __shfl_xor(v, 16, 64);
+      if (n == 0) s_sum[(wave * C::kSubs + sub) * 32 + elem_of(i, g2)] = v;
+    }
   __syncthreads();
   float* out = scores + (static_cast<int64_t>(b) * kv.num_kv_heads + g) * score_stride;
-  if (tid < 128 && t_begin + tid < sh.len) out[t_begin + tid] = s_sum[tid] / static_cast<float>(sh.rows);
+  if (tid < C::kTokens && t_begin + tid < sh.len) out[t_begin + tid] = s_sum[tid] / static_cast<float>(sh.rows);
 }
 
 // ------------------------------------------------------------------ host --
 struct TreePlan {
-  int rt, ts, ranges, tiles_max;
+  int rt, ts, ranges, steps_max;
   int64_t slots;
 };
 
@@ -604,8 +734,8 @@ TreePlan plan_of(const KvView& kv, int max_nodes, bool f32) {
     p.ts = groups <= 1 ? 128 : 64;
     per_cu = groups <= 4 ? 2 : 1;
   }
-  p.tiles_max = (rows + p.rt - 1) / p.rt;
-  const int64_t most = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * p.tiles_max * ((kv.max_seq_len + p.ts - 1) / p.ts);
+  p.steps_max = (kv.max_seq_len + p.ts - 1) / p.ts;
+  const int64_t most = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * ((rows + p.rt - 1) / p.rt) * p.steps_max;
   p.ranges = static_cast<int>(std::min<int64_t>(most, static_cast<int64_t>(per_cu) * num_cus()));
   p.slots = 2 * static_cast<int64_t>(p.ranges);
   return p;
@@ -640,14 +770,16 @@ hipError_t launch_tree(const TreeParams& p, const TreePlan& plan, const TreeArgs
     KernelTimer timer("tree_pass", s);
     hipLaunchKernelGGL((tree_pass<C>), dim3(p.ranges), dim3(C::kThreads), 0, s, p);
   }
-  {
+  if (plan.steps_max > 1 && p.ranges > 1) {
     KernelTimer timer("tree_merge", s);
-    hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT>), dim3(p.kv.num_kv_heads * plan.tiles_max, p.kv.batch, C::RT / 32), dim3(256), 0, s, p,
-                       plan.tiles_max);
+    constexpr int kRows = 256 / (C::D / 4);
+    const int rows = std::min(C::RT, p.max_nodes * p.group);
+    hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT>), dim3(p.ranges - 1, (rows + kRows - 1) / kRows), dim3(256), 0, s, p);
   }
   if (t.scores) {
+    using S = ScoreCfg<C::D, C::KV, C::E::kF32>;
     KernelTimer timer("tree_scores", s);
-    hipLaunchKernelGGL((tree_scores<C::D, C::KV, C::E::kF32>), dim3((p.kv.max_seq_len + 127) / 128, p.kv.num_kv_heads, p.kv.batch), dim3(256), 0, s, p, t.scores,
+    hipLaunchKernelGGL((tree_scores<S>), dim3((p.kv.max_seq_len + S::kTokens - 1) / S::kTokens, p.kv.num_kv_heads, p.kv.batch), dim3(256), 0, s, p, t.scores,
                        t.score_stride);
   }
   return hipGetLastError();
