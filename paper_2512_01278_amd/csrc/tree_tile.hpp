@@ -81,6 +81,15 @@ struct EngineBf16 {
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const u32x4*>(p + 32 * s)), f.q[s], acc, 0, 0, 0);
     return acc;
   }
+  // the same with the roles exchanged: element i is row elem_of(i, g), and a lane's column is a token
+  static __device__ __forceinline__ f32x16 qk_token(const uint8_t* k, const Query& f, int lane) {
+    const uint8_t* p = k + (lane & 31) * kKPitch + ((lane >> 5) << 4);
+    f32x16 acc = {};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[s], as_bf16x8(*reinterpret_cast<const u32x4*>(p + 32 * s)), acc, 0, 0, 0);
+    return acc;
+  }
   // ds_read_b64_tr_b16: within 16 lanes, lane 4k+a gives the address of 4 dims of token k, and lane m receives dim m of the four tokens
   static __device__ __forceinline__ void pv(const uint8_t* v, const f32x16& p, f32x16 (&o)[D / 32], int lane) {
     const int j = lane & 15, h = (lane >> 4) & 1, g = lane >> 5;
@@ -125,6 +134,17 @@ struct EngineF32 {
       const f32x4 a = *reinterpret_cast<const f32x4*>(p + 32 * s);
 #pragma unroll
       for (int c = 0; c < 4; ++c) acc[c & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c], f.q[s][c], acc[c & 1], 0, 0, 0);
+    }
+    return acc[0] + acc[1];
+  }
+  static __device__ __forceinline__ f32x16 qk_token(const uint8_t* k, const Query& f, int lane) {
+    const uint8_t* p = k + (lane & 31) * kKPitch + ((lane >> 5) << 4);
+    f32x16 acc[2] = {};
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(p + 32 * s);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(f.q[s][c], a[c], acc[c & 1], 0, 0, 0);
     }
     return acc[0] + acc[1];
   }

@@ -86,6 +86,45 @@ __device__ __forceinline__ int wave_inclusive(int v, int lane) {
   return v;
 }
 
+// What a workgroup finds out about its share of the work, every wavefront for itself: 64 requests at a time, a request per lane.
+struct Share {
+  int w, u0, u1;               // its range, first unit and past the last
+  int b, ub;                   // the request that has unit u0, and that request's first unit
+  // units: of a request; prefix: the first workgroup leaves the units before every request, and all of them, there
+  template <typename F>
+  __device__ __forceinline__ Share(int batch, int workgroups, int32_t* prefix, F units) {
+    const int lane = threadIdx.x & 63;
+    int total = 0;
+    for (int c = 0; c < batch; c += 64) total += __shfl(wave_inclusive(c + lane < batch ? units(c + lane) : 0, lane), 63, 64);
+    const Ranges ranges(total, workgroups);
+    // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
+    w = blockIdx.x;
+    if (ranges.n == workgroups && workgroups % 8 == 0) w = (w & 7) * (workgroups >> 3) + (w >> 3);
+    u0 = u1 = b = ub = 0;
+    if (w >= ranges.n) return;
+    u0 = ranges.begin(w);
+    u1 = ranges.begin(w + 1);
+    const bool leaves = prefix && w == 0 && threadIdx.x < 64;
+    bool found = false;
+    int before = 0;
+    for (int c = 0; c < batch; c += 64) {
+      const int mine = c + lane < batch ? units(c + lane) : 0;
+      const int upto = wave_inclusive(mine, lane) + before;
+      if (leaves && c + lane < batch) prefix[c + lane] = upto - mine;
+      const uint64_t after = __ballot(upto > u0);
+      if (!found && after) {
+        const int at = __builtin_ctzll(after);
+        b = c + at;
+        ub = __shfl(upto - mine, at, 64);
+        found = true;
+      }
+      before = __shfl(upto, 63, 64);
+      if (found && !leaves) break;
+    }
+    if (leaves && lane == 0) prefix[batch] = total;
+  }
+};
+
 template <int D_, int KV_, bool F32, int WR_, int WT_, int NS_>
 struct Cfg {
   static constexpr int D = D_, KV = KV_, WR = WR_, WT = WT_, NS = NS_;     // WR x WT wavefronts: groups of 32 rows x groups of tokens
@@ -115,15 +154,15 @@ __device__ __forceinline__ void see_nothing(const TreeParams& a, int b, int node
     for (int r = threadIdx.x; r < rows; r += blockDim.x) a.lse[first + r] = -INFINITY;
 }
 
-// The rows of a tile that a thread carries, between global memory and LDS.
-template <typename C>
+// The rows of a tile that a thread carries, between global memory and LDS.  V: rows of V too.
+template <typename C, bool V>
 struct Carrier {
   using E = typename C::E;
   int64_t base;                // elements: this head's rows in page 0
   const int32_t* table;
   int last;                    // the last token: rows past it are read there
   int pid[C::kLoads];
-  u32x4 k[C::kLoads], v[C::kLoads];
+  u32x4 k[C::kLoads], v[V ? C::kLoads : 1];
   int scale_pid;
   float ks, vs;
 
@@ -147,13 +186,13 @@ struct Carrier {
       for (int u = 0; u < C::kLoads; ++u) {
         const int64_t at = elem(kv, step, u);
         k[u] = load_piece<C::KV>(kv.k_pool, at, true);
-        v[u] = load_piece<C::KV>(kv.v_pool, at, true);
+        if constexpr (V) v[u] = load_piece<C::KV>(kv.v_pool, at, true);
       }
     }
     if (C::kScales) {
       const int64_t at = static_cast<int64_t>(scale_pid) * kv.num_kv_heads + g;
       ks = kv.k_scale[at];
-      vs = kv.v_scale[at];
+      if (V) vs = kv.v_scale[at];
     }
   }
 };
@@ -174,50 +213,20 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   uint8_t* const vtile = smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
 
-  // ---- the plan, by every wavefront ----
-  int total = 0;
+  // contexts without a token have no unit: their rows are shared out among the workgroups
   for (int c = 0; c < kv.batch; c += 64) {
     const int r = c + lane;
     Shape sh = {};
     if (r < kv.batch) sh = shape_of<TS, RT>(a, r);
-    total += __shfl(wave_inclusive(sh.steps * sh.tiles * kv.num_kv_heads, lane), 63, 64);
-    // contexts without a token have no unit: their rows are shared out among the workgroups
-    for (uint64_t none = __ballot(sh.len == 0 && sh.nodes > 0); none; none &= none - 1) {
+    for (uint64_t none = __ballot(r < kv.batch && sh.len == 0 && sh.nodes > 0); none; none &= none - 1) {
       const int at = __builtin_ctzll(none);
       if ((c + at) % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) see_nothing<D>(a, c + at, __shfl(sh.nodes, at, 64));
     }
   }
-  const Ranges ranges(total, a.ranges);
-  // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
-  int w = blockIdx.x;
-  if (ranges.n == a.ranges && a.ranges % 8 == 0) w = (w & 7) * (a.ranges >> 3) + (w >> 3);
-  if (w >= ranges.n) return;
-  const bool leader = w == 0 && wave == 0;               // leaves the prefix for the merge
-  const int u0 = ranges.begin(w), u1 = ranges.begin(w + 1);
-  int b = 0, ub = 0;           // the request at work and its first unit
-  {
-    int before = 0;
-    bool found = false;
-    for (int c = 0; c < kv.batch; c += 64) {
-      const int r = c + lane;
-      const int mine = r < kv.batch ? units_of<TS, RT>(a, r) : 0;
-      const int upto = wave_inclusive(mine, lane) + before;
-      if (leader && r < kv.batch) a.prefix[r] = upto - mine;
-      if (!found) {
-        const uint64_t after = __ballot(upto > u0);
-        if (after) {
-          const int at = __builtin_ctzll(after);
-          b = c + at;
-          ub = __shfl(upto - mine, at, 64);
-          found = true;
-        }
-      }
-      before = __shfl(upto, 63, 64);
-      if (found && !leader) break;
-    }
-    if (leader && lane == 0) a.prefix[kv.batch] = total;
-  }
-  if (total == 0) return;
+  Share share(kv.batch, a.ranges, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); });
+  int b = share.b, ub = share.ub;                        // the request at work and its first unit
+  const int w = share.w, u0 = share.u0, u1 = share.u1;
+  if (u0 == u1) return;
   if (tid < 2) s_bad[0][tid] = 0;
   int parity = 0;              // of the stretch: the other half of s_bad is cleared meanwhile
   __syncthreads();
@@ -252,7 +261,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
     float m_run = -INFINITY, l_run = 0.f;
 
-    Carrier<C> c;
+    Carrier<C, true> c;
     c.base = static_cast<int64_t>(g) * kv.stride_head;
     c.table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
     c.last = sh.len - 1;
@@ -552,165 +561,137 @@ __global__ __launch_bounds__(256) void tree_merge(TreeParams a) {
   }
 }
 
-// ---- the statistic: exp(logit - lse) summed over the rows.  A wavefront keeps the K rows of 64 tokens (32 in fp32) in registers as operands and the
-// query rows pass by, 32 at a time, through LDS, fetched one tile ahead.  64 tokens, as the four wavefronts read each tile of Q whole:
-// 32 KB of LDS reads per 4 x 2 x 32 x 32 x 128 products, half of what the matrix cores take in the time. ----
-template <int D_, int KV_, bool F32>
-struct ScoreCfg {
-  static constexpr int D = D_, KV = KV_;
-  using E = std::conditional_t<F32, EngineF32<D>, EngineBf16<D>>;
-  static constexpr int kSubs = F32 ? 1 : 2, kTokens = 4 * 32 * kSubs;      // tokens of a workgroup
-  static constexpr int kQPieces = D * (F32 ? 4 : 2) / 16;                  // 16-byte pieces of a query row in LDS
-  static constexpr int kQLoads = 32 * kQPieces / 256;
-};
+// ---- the statistic: exp(logit - lse) summed over the rows.  Tiles of K pass as in tree_pass, but with the roles of the product exchanged (A = Q, B = K^T): a
+// lane has one token and 16 of the 32 rows, and sums over rows without asking another lane but its other half.  Wavefronts that have
+// other rows of the same tokens join in LDS.  More rows than a workgroup has (256): again for the next rows, adding to what
+// the same threads wrote before. ----
+// wavefronts per SIMD that the statistic's kernel is compiled for: what the registers allow without spilling
+template <typename C>
+constexpr int score_waves() { return C::E::kF32 || C::WR == 1 ? 2 : C::WR == 8 ? 4 : 3; }
 
 template <typename C>
-__global__ __launch_bounds__(256, 2) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
+__global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
   using E = typename C::E;
-  constexpr int D = C::D, KV = C::KV;
-  __shared__ __attribute__((aligned(16))) uint8_t s_q[2][32 * E::kKPitch];
-  __shared__ float s_sum[C::kTokens];
+  constexpr int TS = C::TS, RT = C::RT;
+  __shared__ __attribute__((aligned(16))) uint8_t ktile[TS * E::kKPitch];
+  __shared__ float s_ks[C::kScales ? TS : 1];
+  __shared__ float s_part[C::WR][TS];
+  __shared__ __attribute__((aligned(16))) float s_y[RT];
+  __shared__ uint64_t s_word[RT];
   const KvView& kv = a.kv;
-  const int b = blockIdx.z, g = blockIdx.y, t_begin = blockIdx.x * C::kTokens;
-  const Shape sh = shape_of<C::kTokens, 32>(a, b);
-  if (t_begin >= sh.len || sh.rows == 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g2 = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % C::WR, wt = wave / C::WR, n = lane & 31, g2 = lane >> 5;
   const float scale2 = kv.sm_scale * kLog2e;
-  const int first_node = sh.len - sh.nodes, t0 = t_begin + wave * 32 * C::kSubs;
+  const Share share(kv.batch, gridDim.x, nullptr, [&](int r) {
+    const Shape sh = shape_of<TS, RT>(a, r);
+    return sh.rows > 0 ? sh.steps * kv.num_kv_heads : 0;
+  });
+  int b = share.b, ub = share.ub;
+  for (int u = share.u0; u < share.u1;) {
+    b = __builtin_amdgcn_readfirstlane(b);
+    const Shape sh = shape_of<TS, RT>(a, b);
+    const int units = sh.rows > 0 ? sh.steps * kv.num_kv_heads : 0;
+    if (u >= ub + units) {
+      ub += units;
+      ++b;
+      continue;
+    }
+    const int g = (u - ub) / sh.steps, s0 = u - ub - g * sh.steps, s1 = min(sh.steps, s0 + share.u1 - u);
+    u += s1 - s0;
+    const int first_node = sh.len - sh.nodes;
+    float* out = scores + (static_cast<int64_t>(b) * kv.num_kv_heads + g) * score_stride;
+    Carrier<C, false> c;
+    c.base = static_cast<int64_t>(g) * kv.stride_head;
+    c.table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
+    c.last = sh.len - 1;
 
-  auto row_at = [&](int row) {                           // of q and lse; row < sh.rows
-    const int node = row / a.group;
-    return (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
-  };
-  // ---- a tile of query rows on its way ----
-  u32x4 q_next[C::kQLoads];
-  float y_next;
-  uint64_t word_next;
-  auto fetch = [&](int r0) {
+    for (int r0 = 0; r0 < sh.rows; r0 += RT) {
+      const int row = r0 + wr * 32 + n;
+      const bool there = row < sh.rows, any_row = r0 + wr * 32 < sh.rows;
+      const int node = there ? row / a.group : 0;
+      const int64_t q_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (there ? row - node * a.group : 0);
+      typename E::Query qf;
+      E::load_query(qf, a.q, q_row, there, a.q_dtype, g2);
+      float mine = there ? a.lse2[q_row] : INFINITY;
+      if (mine == -INFINITY) mine = INFINITY;            // a row that sees nothing has no share
+      const bool ragged = __any(mine == INFINITY);
+      if (wt == 0 && g2 == 0) {
+        s_y[wr * 32 + n] = mine;
+        s_word[wr * 32 + n] = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
+      }
+      if constexpr (!E::kF32) {
+        c.pages(kv, s0);
+        c.fetch(kv, g, s0);
+        if (s0 + 1 < s1) c.pages(kv, s0 + 1);
+      }
+      __syncthreads();
+      float y[16];
 #pragma unroll
-    for (int u = 0; u < C::kQLoads; ++u) {
-      const int e = tid + 256 * u, row = r0 + e / C::kQPieces, piece = e % C::kQPieces;
-      q_next[u] = u32x4{0, 0, 0, 0};
-      if (row < sh.rows) {
-        const int64_t at = row_at(row) * D;
-        if constexpr (E::kF32) {
+      for (int i = 0; i < 16; ++i) y[i] = s_y[wr * 32 + elem_of(i, g2)];
+
+      for (int s = s0; s < s1; ++s) {
+        if constexpr (!E::kF32) {
+          if (c.carries()) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int64_t i = at + 4 * piece + j;
-            q_next[u][j] = __float_as_uint(a.q_dtype == PILLAR_F32 ? Storage<PILLAR_F32>::load(a.q, i) : Storage<PILLAR_BF16>::load(a.q, i));
+            for (int i = 0; i < C::kLoads; ++i) park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + c.row(i) * E::kKPitch, c.piece(i));
           }
+          if (C::kScales && tid < TS) s_ks[tid] = c.ks;
         } else {
-          q_next[u] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + 8 * piece);
+#pragma unroll 4
+          for (int i = 0; i < C::kLoads; ++i) {
+            const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
+            if (c.carries()) {
+              const int64_t at = c.base + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
+                                 c.piece(i) * (16 / kv_bytes<C::KV>());
+              float ks = 1.f;
+              if constexpr (C::KV == PILLAR_FP8_E4M3) ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
+              park_piece<E, C::KV, false>(load_piece<C::KV>(kv.k_pool, at, a.aligned), ks, ktile + r * E::kKPitch, c.piece(i));
+            }
+          }
+        }
+        __syncthreads();
+        if constexpr (!E::kF32) {
+          if (s + 1 < s1) {
+            c.fetch(kv, g, s + 1);
+            if (s + 2 < s1) c.pages(kv, s + 2);
+          }
+        }
+#pragma unroll
+        for (int sub = 0; sub < C::NS; ++sub) {
+          const int at = wt * C::kGroupTokens + 32 * sub, t = s * TS + at + n;
+          float sum = 0.f;
+          if (any_row && t - n < sh.len) {
+            const f32x16 x = E::qk_token(ktile + at * E::kKPitch, qf, lane);
+            const float f = C::kScales ? s_ks[at + n] * scale2 : scale2;
+            if (ragged || t - n + 32 > first_node) {
+              const int j = t - first_node;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const bool vis = j < 0 || (j < sh.nodes && (s_word[wr * 32 + elem_of(i, g2)] >> (j & 63) & 1));
+                const float p = fast_exp2(__builtin_fmaf(x[i], f, -y[i]));
+                sum += vis && y[i] != INFINITY ? p : 0.f;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) sum += fast_exp2(__builtin_fmaf(x[i], f, -y[i]));
+            }
+            sum = other_half_sum(sum);
+          }
+          if (g2 == 0) s_part[wr][at + n] = sum;
+        }
+        __syncthreads();
+        if (tid < TS && s * TS + tid < sh.len) {
+          float sum = s_part[0][tid];
+#pragma unroll
+          for (int i = 1; i < C::WR; ++i) sum += s_part[i][tid];
+          float* to = out + s * TS + tid;
+          if (r0 > 0) sum += *to;
+          *to = r0 + RT >= sh.rows ? sum / static_cast<float>(sh.rows) : sum;
         }
       }
-    }
-    const int row = r0 + n;
-    y_next = INFINITY;
-    word_next = 0;
-    if (row < sh.rows) {
-      y_next = a.lse2[row_at(row)];
-      word_next = a.visible[static_cast<int64_t>(b) * a.max_nodes + row / a.group];
-    }
-  };
-  auto park = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < C::kQLoads; ++u) {
-      const int e = tid + 256 * u;
-      *reinterpret_cast<u32x4*>(s_q[buf] + (e / C::kQPieces) * E::kKPitch + 16 * (e % C::kQPieces)) = q_next[u];
-    }
-  };
-  fetch(0);
-
-  // ---- K rows as operands: of 32 tokens, lane (m, g2) has token m, dims 16 s + 8 g2 .. + 7 (fp32: 8 s + 4 g2 .. + 3) ----
-  typename E::Query k[C::kSubs];
-  float f[C::kSubs];                                     // logit scale of this lane's token ...
-#pragma unroll
-  for (int sub = 0; sub < C::kSubs; ++sub) {
-    int page;
-    const int64_t at = row_offset(kv, b, g, min(t0 + 32 * sub + n, sh.len - 1), &page);
-    f[sub] = 1.f;
-    if constexpr (KV == PILLAR_FP8_E4M3) f[sub] = kv.k_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
-    if constexpr (E::kF32) {
-#pragma unroll
-      for (int s = 0; s < D / 8; ++s)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          k[sub].q[s][c] = Storage<KV>::load(kv.k_pool, at + 8 * s + 4 * g2 + c);
-          if constexpr (KV == PILLAR_FP8_E4M3) k[sub].q[s][c] *= f[sub];
-        }
-      f[sub] = 1.f;
-    } else {
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        if constexpr (KV == PILLAR_BF16) {
-          k[sub].q[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(kv.k_pool) + at + 16 * s + 8 * g2));
-        } else {
-          const u32x2 c = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(kv.k_pool) + at + 16 * s + 8 * g2);
-          k[sub].q[s] = widen_fp8x8(c.x, c.y);
-        }
-      }
+      __syncthreads();                                   // s_y and s_word are about to change
     }
   }
-  float sum[C::kSubs][16], scale[C::kSubs][16];          // ... and of the tokens of its accumulator elements
-#pragma unroll
-  for (int sub = 0; sub < C::kSubs; ++sub)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      sum[sub][i] = 0.f;
-      scale[sub][i] = KV == PILLAR_FP8_E4M3 ? __shfl(f[sub], elem_of(i, g2), 64) * scale2 : scale2;
-    }
-
-  int buf = 0;
-  for (int r0 = 0; r0 < sh.rows; r0 += 32, buf ^= 1) {
-    park(buf);
-    const float y = y_next == -INFINITY ? INFINITY : y_next;       // a row that sees nothing has no share
-    const uint64_t word = word_next;
-    const bool there = r0 + n < sh.rows;
-    __syncthreads();                                     // (the other buffer is read no more: its readers are past this barrier's predecessor)
-    if (r0 + 32 < sh.rows) fetch(r0 + 32);
-    if (t0 >= sh.len) continue;
-    const uint8_t* q = s_q[buf] + n * E::kKPitch + 16 * g2;
-    f32x16 x[C::kSubs] = {};
-    if constexpr (E::kF32) {
-#pragma unroll
-      for (int s = 0; s < D / 8; ++s) {
-        const f32x4 qv = *reinterpret_cast<const f32x4*>(q + 32 * s);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[0].q[s][c], qv[c], x[0], 0, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(q + 32 * s));
-#pragma unroll
-        for (int sub = 0; sub < C::kSubs; ++sub) x[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[sub].q[s], qv, x[sub], 0, 0, 0);
-      }
-    }
-    const bool masked = t0 + 32 * C::kSubs > first_node || r0 + 32 > sh.rows;
-#pragma unroll
-    for (int sub = 0; sub < C::kSubs; ++sub)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float p = fast_exp2(__builtin_fmaf(x[sub][i], scale[sub][i], -y));
-        if (masked) {
-          const int j = t0 + 32 * sub + elem_of(i, g2) - first_node;
-          p = there && (j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1))) ? p : 0.f;
-        }
-        sum[sub][i] += p;
-      }
-  }
-  // over the 32 rows of a half wavefront
-#pragma unroll
-  for (int sub = 0; sub < C::kSubs; ++sub)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = row16_sum(sum[sub][i]);
-      v += __shfl_xor(v, 16, 64);
-      if (n == 0) s_sum[(wave * C::kSubs + sub) * 32 + elem_of(i, g2)] = v;
-    }
-  __syncthreads();
-  float* out = scores + (static_cast<int64_t>(b) * kv.num_kv_heads + g) * score_stride;
-  if (tid < C::kTokens && t_begin + tid < sh.len) out[t_begin + tid] = s_sum[tid] / static_cast<float>(sh.rows);
 }
 
 // ------------------------------------------------------------------ host --
@@ -777,10 +758,10 @@ hipError_t launch_tree(const TreeParams& p, const TreePlan& plan, const TreeArgs
     hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT>), dim3(p.ranges - 1, (rows + kRows - 1) / kRows), dim3(256), 0, s, p);
   }
   if (t.scores) {
-    using S = ScoreCfg<C::D, C::KV, C::E::kF32>;
     KernelTimer timer("tree_scores", s);
-    hipLaunchKernelGGL((tree_scores<S>), dim3((p.kv.max_seq_len + S::kTokens - 1) / S::kTokens, p.kv.num_kv_heads, p.kv.batch), dim3(256), 0, s, p, t.scores,
-                       t.score_stride);
+    const int64_t most = static_cast<int64_t>(p.kv.batch) * p.kv.num_kv_heads * plan.steps_max;
+    const int workgroups = static_cast<int>(std::min<int64_t>(most, score_waves<C>() * 4 / C::kWaves * num_cus()));
+    hipLaunchKernelGGL((tree_scores<C>), dim3(workgroups), dim3(C::kThreads), 0, s, p, t.scores, t.score_stride);
   }
   return hipGetLastError();
 }
