@@ -122,6 +122,12 @@ struct Share {
       if (found && !leaves) break;
     }
     if (leaves && lane == 0) prefix[batch] = total;
+    // (the same in all lanes: kept in scalar registers)
+    w = __builtin_amdgcn_readfirstlane(w);
+    u0 = __builtin_amdgcn_readfirstlane(u0);
+    u1 = __builtin_amdgcn_readfirstlane(u1);
+    b = __builtin_amdgcn_readfirstlane(b);
+    ub = __builtin_amdgcn_readfirstlane(ub);
   }
 };
 
@@ -141,6 +147,13 @@ struct Cfg {
   static constexpr int kLds = kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes;
 };
 
+// Which of 32 tokens a row sees that has `word`, the tree beginning `before` tokens on from the first of them (or -before ahead of it).
+__device__ __forceinline__ uint32_t sees_of(uint64_t word, int before) {
+  if (before >= 32) return ~0u;
+  if (before <= -64) return 0;
+  return before >= 0 ? static_cast<uint32_t>(word << before) | ((1u << before) - 1) : static_cast<uint32_t>(word >> -before);
+}
+
 // Results of the rows of a request that has nothing to see, by a whole workgroup.
 template <int D>
 __device__ __forceinline__ void see_nothing(const TreeParams& a, int b, int nodes) {
@@ -154,39 +167,48 @@ __device__ __forceinline__ void see_nothing(const TreeParams& a, int b, int node
     for (int r = threadIdx.x; r < rows; r += blockDim.x) a.lse[first + r] = -INFINITY;
 }
 
-// The rows of a tile that a thread carries, between global memory and LDS.  V: rows of V too.
+// The pieces of a tile that a thread carries, one place in every kRows-th row, between global memory and LDS.  V: of V too.
 template <typename C, bool V>
 struct Carrier {
   using E = typename C::E;
-  int64_t base;                // elements: this head's rows in page 0
+  static constexpr int kRows = C::kThreads / C::kPieces;
+  const uint8_t* k_rows;       // this head's rows in page 0
+  const uint8_t* v_rows;
   const int32_t* table;
   int last;                    // the last token: rows past it are read there
+  int row0, piece;
   int pid[C::kLoads];
   u32x4 k[C::kLoads], v[V ? C::kLoads : 1];
   int scale_pid;
   float ks, vs;
 
-  static __device__ __forceinline__ int row(int u) { return (threadIdx.x + u * C::kThreads) / C::kPieces; }
-  static __device__ __forceinline__ int piece(int u) { return (threadIdx.x + u * C::kThreads) % C::kPieces; }
-  static __device__ __forceinline__ bool carries() { return C::kAllLoad || threadIdx.x < C::TS * C::kPieces; }
-
+  __device__ __forceinline__ Carrier(const KvView& kv, int b, int g, int len) {
+    const int64_t head = static_cast<int64_t>(g) * kv.stride_head * kv_bytes<C::KV>();
+    k_rows = static_cast<const uint8_t*>(kv.k_pool) + head;
+    v_rows = static_cast<const uint8_t*>(kv.v_pool) + head;
+    table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
+    last = len - 1;
+    row0 = threadIdx.x / C::kPieces;
+    piece = threadIdx.x % C::kPieces;
+  }
+  __device__ __forceinline__ int row(int u) const { return row0 + u * kRows; }
+  __device__ __forceinline__ bool carries() const { return C::kAllLoad || threadIdx.x < C::TS * C::kPieces; }
   __device__ __forceinline__ int token(int step, int r) const { return min(step * C::TS + r, last); }
   __device__ __forceinline__ void pages(const KvView& kv, int step) {
 #pragma unroll
     for (int u = 0; u < C::kLoads; ++u) pid[u] = carries() ? table[token(step, row(u)) >> kv.page_shift] : 0;
     if (C::kScales) scale_pid = table[token(step, min<int>(threadIdx.x, C::TS - 1)) >> kv.page_shift];
   }
-  __device__ __forceinline__ int64_t elem(const KvView& kv, int step, int u) const {
-    return base + static_cast<int64_t>(pid[u]) * kv.stride_page + static_cast<int64_t>(token(step, row(u)) & (kv.page_size - 1)) * kv.stride_slot +
-           piece(u) * (16 / kv_bytes<C::KV>());
-  }
+  // (strides below 2^32 bytes: a row's offset is two products of 32 bits)
   __device__ __forceinline__ void fetch(const KvView& kv, int g, int step) {
+    const uint32_t page_bytes = static_cast<uint32_t>(kv.stride_page * kv_bytes<C::KV>()), slot_bytes = static_cast<uint32_t>(kv.stride_slot * kv_bytes<C::KV>());
     if (carries()) {
 #pragma unroll
       for (int u = 0; u < C::kLoads; ++u) {
-        const int64_t at = elem(kv, step, u);
-        k[u] = load_piece<C::KV>(kv.k_pool, at, true);
-        if constexpr (V) v[u] = load_piece<C::KV>(kv.v_pool, at, true);
+        const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(pid[u])) * page_bytes +
+                            static_cast<uint64_t>(static_cast<uint32_t>(token(step, row(u)) & (kv.page_size - 1))) * slot_bytes + 16 * piece;
+        k[u] = *reinterpret_cast<const u32x4*>(k_rows + at);
+        if constexpr (V) v[u] = *reinterpret_cast<const u32x4*>(v_rows + at);
       }
     }
     if (C::kScales) {
@@ -254,17 +276,14 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     const int64_t out_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + head;
     typename E::Query qf;
     E::load_query(qf, a.q, out_row, there, a.q_dtype, g2);
-    const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
+    const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] & (~0ull >> (64 - sh.nodes)) : 0;
     const int first_node = sh.len - sh.nodes;            // token of node 0 (below 0: it is not in the cache)
     f32x16 o[D / 32];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
     float m_run = -INFINITY, l_run = 0.f;
 
-    Carrier<C, true> c;
-    c.base = static_cast<int64_t>(g) * kv.stride_head;
-    c.table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
-    c.last = sh.len - 1;
+    Carrier<C, true> c(kv, b, g, sh.len);
     if constexpr (!E::kF32) {
       c.pages(kv, s0);
       c.fetch(kv, g, s0);
@@ -290,8 +309,8 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
 #pragma unroll
           for (int i = 0; i < C::kLoads; ++i) {
             const int r = c.row(i);
-            park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + r * E::kKPitch, c.piece(i));
-            park_v(c.v[i], 1.f, s, r, c.piece(i), tail);
+            park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + r * E::kKPitch, c.piece);
+            park_v(c.v[i], 1.f, s, r, c.piece, tail);
           }
         }
         if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
@@ -300,16 +319,16 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
         for (int i = 0; i < C::kLoads; ++i) {
           const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
           if (c.carries()) {
-            const int64_t at = c.base + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
-                               c.piece(i) * (16 / kv_bytes<C::KV>());
+            const int64_t at = static_cast<int64_t>(g) * kv.stride_head + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
+                               c.piece * (16 / kv_bytes<C::KV>());
             const u32x4 kx = load_piece<C::KV>(kv.k_pool, at, a.aligned), vx = load_piece<C::KV>(kv.v_pool, at, a.aligned);
             float ks = 1.f, vs = 1.f;
             if constexpr (C::KV == PILLAR_FP8_E4M3) {
               ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
               vs = kv.v_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
             }
-            park_piece<E, C::KV, false>(kx, ks, ktile + r * E::kKPitch, c.piece(i));
-            park_v(vx, vs, s, r, c.piece(i), tail);
+            park_piece<E, C::KV, false>(kx, ks, ktile + r * E::kKPitch, c.piece);
+            park_v(vx, vs, s, r, c.piece, tail);
           }
         }
       }
@@ -324,68 +343,72 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
 
       // ---- 32 tokens at a time ----
       if (any_row) {
+        const int at = wt * C::kGroupTokens, t0 = s * TS + at;
+        const bool masked = t0 + C::kGroupTokens > first_node;
+        f32x16 x[C::NS];
 #pragma unroll
         for (int sub = 0; sub < C::NS; ++sub) {
-          const int at = wt * C::kGroupTokens + 32 * sub, t0 = s * TS + at;
-          if (t0 >= sh.len) break;
-          const bool masked = t0 + 32 > first_node;
-          f32x16 x = E::qk(ktile + at * E::kKPitch, qf, lane);
+          x[sub] = E::qk(ktile + (at + 32 * sub) * E::kKPitch, qf, lane);
           if constexpr (C::kScales) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(s_ks + at + elem_of(i, g2));
+              const f32x4 f = *reinterpret_cast<const f32x4*>(s_ks + at + 32 * sub + elem_of(i, g2));
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[i + j] *= f[j];
+              for (int j = 0; j < 4; ++j) x[sub][i + j] *= f[j];
             }
           }
-          uint32_t sees = 0;                             // bit i: this row sees the token of element i
-          if (masked) {
+        }
+        uint32_t sees[C::NS];                            // bit elem_of(i, 0): this row sees the token of element i
+        if (masked) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = t0 + elem_of(i, g2) - first_node;
-              const bool vis = j < 0 || (j < sh.nodes && ((word >> (j & 63)) & 1));
-              sees |= static_cast<uint32_t>(vis) << i;
-              x[i] = vis ? x[i] : -INFINITY;
-            }
+          for (int sub = 0; sub < C::NS; ++sub) {
+            sees[sub] = sees_of(word, first_node - (t0 + 32 * sub)) >> (4 * g2);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[sub][i] = (sees[sub] >> elem_of(i, 0) & 1u) ? x[sub][i] : -INFINITY;
           }
-          float top = x[0];
+        }
+        float top = x[0][0];
 #pragma unroll
-          for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-          top = other_half_max(top) * scale2;
-          // The maximum that exponentials are relative to moves only when a logit exceeds it by more than 8 (in log2 units): P stays below
-          // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.
-          if (__any(top > m_run + 8.f)) {
-            const float m_new = fmaxf(m_run, top);
-            const float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
-            m_run = m_new;
-            l_run *= f;
+        for (int sub = 0; sub < C::NS; ++sub)
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db)
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, x[sub][i]);
+        top = other_half_max(top) * scale2;
+        // The maximum that exponentials are relative to moves only when a logit exceeds it by more than 8 (in log2 units): P stays below
+        // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.
+        if (__any(top > m_run + 8.f)) {
+          const float m_new = fmaxf(m_run, top);
+          const float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
+          m_run = m_new;
+          l_run *= f;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[db][i] *= f;
-          }
-          const float m_use = m_run == -INFINITY ? 0.f : m_run;
-          float sum = 0.f;
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] *= f;
+        }
+        const float m_use = m_run == -INFINITY ? 0.f : m_run;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int sub = 0; sub < C::NS; ++sub) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            x[i] = fast_exp2(__builtin_fmaf(x[i], scale2, -m_use));
-            sum += x[i];
+            x[sub][i] = fast_exp2(__builtin_fmaf(x[sub][i], scale2, -m_use));
+            sum[i & 1] += x[sub][i];
           }
-          l_run += sum;
           if constexpr (C::kScales) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(s_vs + at + elem_of(i, g2));
+              const f32x4 f = *reinterpret_cast<const f32x4*>(s_vs + at + 32 * sub + elem_of(i, g2));
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[i + j] *= f[j];
+              for (int j = 0; j < 4; ++j) x[sub][i + j] *= f[j];
             }
             if (masked) {                                // (the scale of a page that no row sees may be anything)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = (sees >> i & 1u) ? x[i] : 0.f;
+              for (int i = 0; i < 16; ++i) x[sub][i] = (sees[sub] >> elem_of(i, 0) & 1u) ? x[sub][i] : 0.f;
             }
           }
-          E::pv(vtile + at * E::kVPitch, x, o, lane);
+          E::pv(vtile + (at + 32 * sub) * E::kVPitch, x[sub], o, lane);
         }
+        l_run += sum[0] + sum[1];
       }
       __syncthreads();
     }
@@ -600,10 +623,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
     u += s1 - s0;
     const int first_node = sh.len - sh.nodes;
     float* out = scores + (static_cast<int64_t>(b) * kv.num_kv_heads + g) * score_stride;
-    Carrier<C, false> c;
-    c.base = static_cast<int64_t>(g) * kv.stride_head;
-    c.table = kv.block_table + static_cast<int64_t>(b) * kv.block_table_stride;
-    c.last = sh.len - 1;
+    Carrier<C, false> c(kv, b, g, sh.len);
 
     for (int r0 = 0; r0 < sh.rows; r0 += RT) {
       const int row = r0 + wr * 32 + n;
@@ -633,7 +653,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
         if constexpr (!E::kF32) {
           if (c.carries()) {
 #pragma unroll
-            for (int i = 0; i < C::kLoads; ++i) park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + c.row(i) * E::kKPitch, c.piece(i));
+            for (int i = 0; i < C::kLoads; ++i) park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + c.row(i) * E::kKPitch, c.piece);
           }
           if (C::kScales && tid < TS) s_ks[tid] = c.ks;
         } else {
@@ -641,11 +661,11 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
           for (int i = 0; i < C::kLoads; ++i) {
             const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
             if (c.carries()) {
-              const int64_t at = c.base + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
-                                 c.piece(i) * (16 / kv_bytes<C::KV>());
+              const int64_t at = static_cast<int64_t>(g) * kv.stride_head + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
+                                 c.piece * (16 / kv_bytes<C::KV>());
               float ks = 1.f;
               if constexpr (C::KV == PILLAR_FP8_E4M3) ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
-              park_piece<E, C::KV, false>(load_piece<C::KV>(kv.k_pool, at, a.aligned), ks, ktile + r * E::kKPitch, c.piece(i));
+              park_piece<E, C::KV, false>(load_piece<C::KV>(kv.k_pool, at, a.aligned), ks, ktile + r * E::kKPitch, c.piece);
             }
           }
         }
@@ -738,6 +758,12 @@ TreeWs carve(const KvView& kv, int max_nodes, const TreePlan& p) {
   return w;
 }
 
+// the matrix-core kernels work out a row's offset from strides of 32 bits
+bool strides_fit(const KvView& kv, int kv_dtype) {
+  const int64_t most = (int64_t{1} << 32) / (kv_dtype == PILLAR_BF16 ? 2 : 1) - 1;
+  return kv.stride_page <= most && kv.stride_slot <= most;
+}
+
 bool rows_aligned(const KvView& kv, int kv_dtype) {
   const int64_t per = kv_dtype == PILLAR_F32 ? 4 : kv_dtype == PILLAR_BF16 ? 8 : 16;       // elements per 16 bytes
   return kv.stride_page % per == 0 && kv.stride_head % per == 0 && kv.stride_slot % per == 0 &&
@@ -798,7 +824,7 @@ bool verify_tree_counts(const KvView& kv, int max_nodes) {
 
 hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
   const KvView& kv = t.kv;
-  const bool f32 = t.generic || t.q_dtype != PILLAR_BF16 || t.kv_dtype == PILLAR_F32 || !rows_aligned(kv, t.kv_dtype) ||
+  const bool f32 = t.generic || t.q_dtype != PILLAR_BF16 || t.kv_dtype == PILLAR_F32 || !rows_aligned(kv, t.kv_dtype) || !strides_fit(kv, t.kv_dtype) ||
                    ((reinterpret_cast<uintptr_t>(t.q) | reinterpret_cast<uintptr_t>(t.out)) & 15u) != 0;
   const TreePlan plan = plan_of(kv, t.max_nodes, f32);
   const TreeWs w = carve(kv, t.max_nodes, plan);
