@@ -68,7 +68,7 @@ struct EngineBf16 {
   struct Query { bf16x8 q[D / 16]; };
 
   // rows: Q[row][0..D-1] of this lane's row, or null (zeros)
-  static __device__ __forceinline__ void load_query(Query& f, const void* q, int64_t row, bool there, int, int g) {
+  static __device__ __forceinline__ void load_query(Query& f, const void* q, int64_t row, bool there, int, bool, int g) {
     const uint16_t* p = static_cast<const uint16_t*>(q) + row * D + 8 * g;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) f.q[s] = as_bf16x8(there ? *reinterpret_cast<const u32x4*>(p + 16 * s) : u32x4{0, 0, 0, 0});
@@ -117,14 +117,22 @@ struct EngineF32 {
   static constexpr int kKPitch = 4 * (D + 4), kVPitch = 4 * (D + 8);
   struct Query { f32x4 q[D / 8]; };
 
-  static __device__ __forceinline__ void load_query(Query& f, const void* q, int64_t row, bool there, int q_dtype, int g) {
+  // dense: rows of q are multiples of 16 bytes
+  static __device__ __forceinline__ void load_query(Query& f, const void* q, int64_t row, bool there, int q_dtype, bool dense, int g) {
+    const int64_t first = row * D + 4 * g;
+    if (!there) {
 #pragma unroll
-    for (int s = 0; s < D / 8; ++s)
+      for (int s = 0; s < D / 8; ++s) f.q[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    } else if (q_dtype == PILLAR_F32 && dense) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int64_t at = row * D + 8 * s + 4 * g + c;
-        f.q[s][c] = !there ? 0.f : q_dtype == PILLAR_F32 ? Storage<PILLAR_F32>::load(q, at) : Storage<PILLAR_BF16>::load(q, at);
-      }
+      for (int s = 0; s < D / 8; ++s) f.q[s] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(q) + first + 8 * s);
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 8; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          f.q[s][c] = q_dtype == PILLAR_F32 ? Storage<PILLAR_F32>::load(q, first + 8 * s + c) : Storage<PILLAR_BF16>::load(q, first + 8 * s + c);
+    }
   }
   static __device__ __forceinline__ f32x16 qk(const uint8_t* k, const Query& f, int lane) {
     const uint8_t* p = k + (lane & 31) * kKPitch + ((lane >> 5) << 4);

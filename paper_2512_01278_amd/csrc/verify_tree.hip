@@ -33,7 +33,8 @@ struct TreeParams {
   void* out;
   float* lse;                  // may be null
   int32_t max_nodes, group, q_dtype;
-  bool aligned;                // cache rows can be read 16 bytes at a time
+  bool aligned;                // cache rows can be read 16 bytes at a time,
+  bool dense;                  // rows of q and out too
   // workspace
   int32_t* prefix;             // [B+1] units before a request, and all of them
   float* part_ml;              // [slots][RT][2]
@@ -77,12 +78,14 @@ struct Ranges {
   }
 };
 
-__device__ __forceinline__ int wave_inclusive(int v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(v, o, 64);
-    if (lane >= o) v += x;
-  }
+// running sum over the lanes of a wavefront
+__device__ __forceinline__ int wave_inclusive(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8: within rows of 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);    // row_bcast 15: a row's sum into the next, rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // row_bcast 31: of the first two into the others
   return v;
 }
 
@@ -90,12 +93,17 @@ __device__ __forceinline__ int wave_inclusive(int v, int lane) {
 struct Share {
   int w, u0, u1;               // its range, first unit and past the last
   int b, ub;                   // the request that has unit u0, and that request's first unit
-  // units: of a request; prefix: the first workgroup leaves the units before every request, and all of them, there
-  template <typename F>
-  __device__ __forceinline__ Share(int batch, int workgroups, int32_t* prefix, F units) {
+  // units: of a request; each(c): called for every 64 requests; prefix: the first workgroup leaves the units before every request, and all of them, there
+  template <typename F, typename Each>
+  __device__ __forceinline__ Share(int batch, int workgroups, int32_t* prefix, F units, Each each) {
     const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int c = 0; c < batch; c += 64) total += __shfl(wave_inclusive(c + lane < batch ? units(c + lane) : 0, lane), 63, 64);
+    int total = 0, mine = 0, upto = 0;
+    for (int c = 0; c < batch; c += 64) {
+      mine = c + lane < batch ? units(c + lane) : 0;
+      upto = total + wave_inclusive(mine);
+      total = __builtin_amdgcn_readlane(upto, 63);
+      each(c);
+    }
     const Ranges ranges(total, workgroups);
     // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
     w = blockIdx.x;
@@ -108,17 +116,19 @@ struct Share {
     bool found = false;
     int before = 0;
     for (int c = 0; c < batch; c += 64) {
-      const int mine = c + lane < batch ? units(c + lane) : 0;
-      const int upto = wave_inclusive(mine, lane) + before;
+      if (batch > 64) {                                  // (else both are still there)
+        mine = c + lane < batch ? units(c + lane) : 0;
+        upto = before + wave_inclusive(mine);
+        before = __builtin_amdgcn_readlane(upto, 63);
+      }
       if (leaves && c + lane < batch) prefix[c + lane] = upto - mine;
       const uint64_t after = __ballot(upto > u0);
       if (!found && after) {
         const int at = __builtin_ctzll(after);
         b = c + at;
-        ub = __shfl(upto - mine, at, 64);
+        ub = __builtin_amdgcn_readlane(upto - mine, at);
         found = true;
       }
-      before = __shfl(upto, 63, 64);
       if (found && !leaves) break;
     }
     if (leaves && lane == 0) prefix[batch] = total;
@@ -153,6 +163,30 @@ __device__ __forceinline__ uint32_t sees_of(uint64_t word, int before) {
   if (before >= 32) return ~0u;
   if (before <= -64) return 0;
   return before >= 0 ? static_cast<uint32_t>(word << before) | ((1u << before) - 1) : static_cast<uint32_t>(word >> -before);
+}
+
+// four dims of an output row
+template <int D>
+__device__ __forceinline__ void store_dims(const TreeParams& a, int64_t row, int dim, f32x4 x) {
+  const int64_t at = row * D + dim;
+  if (a.q_dtype == PILLAR_F32) {
+    if (a.dense) {
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = x;
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) Storage<PILLAR_F32>::store(a.out, at + j, x[j]);
+  } else {
+    if (a.dense) {
+      u32x2 y;
+      y.x = f32_to_bf16(x[0]) | static_cast<uint32_t>(f32_to_bf16(x[1])) << 16;
+      y.y = f32_to_bf16(x[2]) | static_cast<uint32_t>(f32_to_bf16(x[3])) << 16;
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = y;
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) Storage<PILLAR_BF16>::store(a.out, at + j, x[j]);
+  }
 }
 
 // Results of the rows of a request that has nothing to see, by a whole workgroup.
@@ -240,17 +274,13 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   uint8_t* const vtile = smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
 
-  // contexts without a token have no unit: their rows are shared out among the workgroups
-  for (int c = 0; c < kv.batch; c += 64) {
-    const int r = c + lane;
-    Shape sh = {};
-    if (r < kv.batch) sh = shape_of<TS, RT>(a, r);
-    for (uint64_t none = __ballot(r < kv.batch && sh.len == 0 && sh.nodes > 0); none; none &= none - 1) {
-      const int at = __builtin_ctzll(none);
-      if ((c + at) % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) see_nothing<D>(a, c + at, __shfl(sh.nodes, at, 64));
+  const Share share(kv.batch, a.ranges, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
+    // contexts without a token have no unit: their rows are shared out among the workgroups
+    for (uint64_t none = __ballot(c + lane < kv.batch && kv.seq_lens[min(c + lane, kv.batch - 1)] <= 0); none; none &= none - 1) {
+      const int r = c + __builtin_ctzll(none);
+      if (r % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) see_nothing<D>(a, r, shape_of<TS, RT>(a, r).nodes);
     }
-  }
-  Share share(kv.batch, a.ranges, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); });
+  });
   int b = share.b, ub = share.ub;                        // the request at work and its first unit
   const int w = share.w, u0 = share.u0, u1 = share.u1;
   if (u0 == u1) return;
@@ -280,7 +310,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     const int node = there ? row / a.group : 0, head = g * a.group + (there ? row - node * a.group : 0);
     const int64_t out_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + head;
     typename E::Query qf;
-    E::load_query(qf, a.q, out_row, there, a.q_dtype, g2);
+    E::load_query(qf, a.q, out_row, there, a.q_dtype, a.dense, g2);
     const uint64_t word = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] & (~0ull >> (64 - sh.nodes)) : 0;
     const int first_node = sh.len - sh.nodes;            // token of node 0 (below 0: it is not in the cache)
     f32x16 o[D / 32];
@@ -470,17 +500,8 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     auto leave_dims = [&](int64_t to_row, int in_tile, int dim, f32x4 x, float inv) {
       if (!whole) {
         *reinterpret_cast<f32x4*>(a.part_o + (static_cast<int64_t>(slot) * RT + in_tile) * D + dim) = x;
-      } else if (!E::kF32) {
-        u32x2 y;
-        y.x = f32_to_bf16(x[0] * inv) | static_cast<uint32_t>(f32_to_bf16(x[1] * inv)) << 16;
-        y.y = f32_to_bf16(x[2] * inv) | static_cast<uint32_t>(f32_to_bf16(x[3] * inv)) << 16;
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_row * D + dim) = y;
       } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to_row * D + dim + j, x[j] * inv);
-          else Storage<PILLAR_BF16>::store(a.out, to_row * D + dim + j, x[j] * inv);
-        }
+        store_dims<D>(a, to_row, dim, x * inv);
       }
     };
     if constexpr (C::WT == 1) {
@@ -532,10 +553,10 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
 
 // ---- joins what several ranges left of a tile.  A tile is cut where a range begins inside it, so there is a row of workgroups for each range, which
 // do nothing unless theirs is the first to begin inside its tile.  A row has D/4 lanes: they fetch (m, l) of as many partials side by
-// side, then the partials of O, eight under way. ----
-template <int D, int TS, int RT>
-__global__ __launch_bounds__(256) void tree_merge(TreeParams a) {
-  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+// side, and the partials of O kAhead at a time. ----
+template <int D, int TS, int RT, int kAhead>
+__global__ __launch_bounds__(128) void tree_merge(TreeParams a) {
+  constexpr int kLanes = D / 4, kRows = 128 / kLanes;
   const KvView& kv = a.kv;
   const int lane = threadIdx.x & 63, part = threadIdx.x % kLanes;
   const Ranges ranges(a.prefix[kv.batch], a.ranges);
@@ -558,49 +579,47 @@ __global__ __launch_bounds__(256) void tree_merge(TreeParams a) {
   if (w0 != w - 1) return;
   const int first_slot = 2 * w0 + (ranges.begin(w0) < first ? 1 : 0);      // the others begin their range
   const int g = index / sh.tiles, tile = index - g * sh.tiles;
-  const int r = blockIdx.y * kRows + threadIdx.x / kLanes, row = tile * RT + r;
-  if (row >= sh.rows) return;
-  const int count = w1 - w0 + 1;
-  auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? first_slot : 2 * (w0 + i)) * RT + r; };
-  float m = -INFINITY;
-  for (int c = 0; c < count; c += kLanes)
-    if (c + part < count) m = fmaxf(m, a.part_ml[2 * at(c + part)]);
+  const int count = w1 - w0 + 1, r_end = min(RT, sh.rows - tile * RT);
+  for (int r = blockIdx.y * kRows + threadIdx.x / kLanes; r < r_end; r += gridDim.y * kRows) {
+    const int row = tile * RT + r;
+    auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? first_slot : 2 * (w0 + i)) * RT + r; };
+    f32x4 o[kAhead];
+    auto fetch = [&](int i) {
 #pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kLanes));
-  const float m_use = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  f32x4 x = {};
-  for (int c = 0; c < count; c += kLanes) {
-    float f = 0.f;
-    if (c + part < count) {
-      const float* ml = a.part_ml + 2 * at(c + part);
-      f = fast_exp2(ml[0] - m_use);
-      l += ml[1] * f;
+      for (int j = 0; j < kAhead; ++j) o[j] = *reinterpret_cast<const f32x4*>(a.part_o + at(min(i + j, count - 1)) * D + 4 * part);
+    };
+    fetch(0);                                            // (beside the (m, l) that it is weighed by)
+    float m = -INFINITY;
+    for (int c = part; c < count; c += kLanes) m = fmaxf(m, a.part_ml[2 * at(c)]);
+#pragma unroll
+    for (int k = kLanes / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k, kLanes));
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float l = 0.f, f = 0.f;
+    f32x4 x = {};
+    for (int i = 0; i < count; i += kAhead) {
+      if (i % kLanes == 0) {                             // the weights of the next partials, one to a lane
+        f = 0.f;
+        if (i + part < count) {
+          const float* ml = a.part_ml + 2 * at(i + part);
+          f = fast_exp2(ml[0] - m_use);
+          l += ml[1] * f;
+        }
+      }
+      if (i > 0) fetch(i);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < count) x += o[j] * __shfl(f, i % kLanes + j, kLanes);
     }
-    const int here = min(kLanes, count - c);
-    for (int i = 0; i < here; i += 8) {
-      f32x4 o[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = *reinterpret_cast<const f32x4*>(a.part_o + at(min(c + i + j, count - 1)) * D + 4 * part);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (i + j < here) x += o[j] * __shfl(f, i + j, kLanes);
+    for (int k = kLanes / 2; k > 0; k >>= 1) l += __shfl_xor(l, k, kLanes);
+    const int node = row / a.group;
+    const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
+    if (part == 0) {
+      const float y = l == 0.f ? -INFINITY : m + log2f(l);
+      if (a.lse) a.lse[to] = y * kLn2;
+      if (a.lse2) a.lse2[to] = y;
     }
-  }
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, kLanes);
-  const int node = row / a.group;
-  const int64_t to = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (row - node * a.group);
-  if (part == 0) {
-    const float y = l == 0.f ? -INFINITY : m + log2f(l);
-    if (a.lse) a.lse[to] = y * kLn2;
-    if (a.lse2) a.lse2[to] = y;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, to * D + 4 * part + j, x[j] * inv);
-    else Storage<PILLAR_BF16>::store(a.out, to * D + 4 * part + j, x[j] * inv);
+    store_dims<D>(a, to, 4 * part, x * (l == 0.f ? 0.f : 1.f / l));
   }
 }
 
@@ -628,7 +647,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
   const Share share(kv.batch, gridDim.x, nullptr, [&](int r) {
     const Shape sh = shape_of<TS, RT>(a, r);
     return sh.rows > 0 ? sh.steps * kv.num_kv_heads : 0;
-  });
+  }, [](int) {});
   int b = share.b, ub = share.ub;
   for (int u = share.u0; u < share.u1;) {
     b = __builtin_amdgcn_readfirstlane(b);
@@ -651,7 +670,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
       const int node = there ? row / a.group : 0;
       const int64_t q_row = (static_cast<int64_t>(b) * a.max_nodes + node) * kv.num_q_heads + g * a.group + (there ? row - node * a.group : 0);
       typename E::Query qf;
-      E::load_query(qf, a.q, q_row, there, a.q_dtype, g2);
+      E::load_query(qf, a.q, q_row, there, a.q_dtype, a.dense, g2);
       float mine = there ? a.lse2[q_row] : INFINITY;
       if (mine == -INFINITY) mine = INFINITY;            // a row that sees nothing has no share
       const bool ragged = __any(mine == INFINITY);
@@ -737,7 +756,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
 // ------------------------------------------------------------------ host --
 struct TreePlan {
   int rt, ts, ranges, steps_max;
-  int64_t slots;
+  int64_t tiles, slots;        // (request, head, tile of rows) there may be; partial results
 };
 
 // Wavefronts side by side on the rows: as many groups of 32 as there are rows, up to 8; the others of a workgroup of four take other tokens.
@@ -756,8 +775,8 @@ TreePlan plan_of(const KvView& kv, int max_nodes, bool f32) {
     per_cu = groups <= 4 ? 2 : 1;
   }
   p.steps_max = (kv.max_seq_len + p.ts - 1) / p.ts;
-  const int64_t most = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * ((rows + p.rt - 1) / p.rt) * p.steps_max;
-  p.ranges = static_cast<int>(std::min<int64_t>(most, static_cast<int64_t>(per_cu) * num_cus()));
+  p.tiles = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * ((rows + p.rt - 1) / p.rt);
+  p.ranges = static_cast<int>(std::min<int64_t>(p.tiles * p.steps_max, static_cast<int64_t>(per_cu) * num_cus()));
   p.slots = 2 * static_cast<int64_t>(p.ranges);
   return p;
 }
@@ -799,9 +818,16 @@ hipError_t launch_tree(const TreeParams& p, const TreePlan& plan, const TreeArgs
   }
   if (plan.steps_max > 1 && p.ranges > 1) {
     KernelTimer timer("tree_merge", s);
-    constexpr int kRows = 256 / (C::D / 4);
+    constexpr int kThreads = 128, kRows = kThreads / (C::D / 4);
     const int rows = std::min(C::RT, p.max_nodes * p.group);
-    hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT>), dim3(p.ranges - 1, (rows + kRows - 1) / kRows), dim3(256), 0, s, p);
+    // of the workgroups that find work (one of the ranges of a tile) no more than the chip holds at once: 32 requests of 4096 tokens 17 / 15 us,
+    // 128 of 1-8 K 24 / 18
+    const int64_t busy = std::min<int64_t>(p.ranges - 1, plan.tiles);
+    const int room = static_cast<int>(std::max<int64_t>(1, 16 * num_cus() / busy));
+    const dim3 grid(p.ranges - 1, std::min(room, (rows + kRows - 1) / kRows));
+    // many ranges to a tile: many partials at once, which take registers that two or three to a tile would miss (16 for all: 15 / 20 and 18 / 30 us)
+    if (p.ranges > 4 * plan.tiles) hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT, 16>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<C::D, C::TS, C::RT, 4>), grid, dim3(kThreads), 0, s, p);
   }
   if (t.scores) {
     KernelTimer timer("tree_scores", s);
@@ -850,8 +876,8 @@ bool verify_tree_counts(const KvView& kv, int max_nodes) {
 
 hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
   const KvView& kv = t.kv;
-  const bool f32 = t.generic || t.q_dtype != PILLAR_BF16 || t.kv_dtype == PILLAR_F32 || !rows_aligned(kv, t.kv_dtype) || !strides_fit(kv, t.kv_dtype) ||
-                   ((reinterpret_cast<uintptr_t>(t.q) | reinterpret_cast<uintptr_t>(t.out)) & 15u) != 0;
+  const bool dense = ((reinterpret_cast<uintptr_t>(t.q) | reinterpret_cast<uintptr_t>(t.out)) & 15u) == 0;
+  const bool f32 = t.generic || t.q_dtype != PILLAR_BF16 || t.kv_dtype == PILLAR_F32 || !rows_aligned(kv, t.kv_dtype) || !strides_fit(kv, t.kv_dtype) || !dense;
   const TreePlan plan = plan_of(kv, t.max_nodes, f32);
   const TreeWs w = carve(kv, t.max_nodes, plan);
   char* ws = static_cast<char*>(t.workspace);
@@ -866,6 +892,7 @@ hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
   p.group = kv.num_q_heads / kv.num_kv_heads;
   p.q_dtype = t.q_dtype;
   p.aligned = rows_aligned(kv, t.kv_dtype);
+  p.dense = dense;
   p.prefix = reinterpret_cast<int32_t*>(ws);
   p.part_ml = reinterpret_cast<float*>(ws + w.ml);
   p.part_o = reinterpret_cast<float*>(ws + w.o);
