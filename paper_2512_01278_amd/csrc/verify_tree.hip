@@ -40,7 +40,7 @@ struct TreeParams {
   float* part_ml;              // [slots][RT][2]
   float* part_o;               // [slots][RT][D]
   float* lse2;                 // [B][max_nodes][Hq], in log2 units; only with scores
-  int32_t ranges;              // workgroups of the pass
+  int32_t ranges, few;         // workgroups of the pass; of those, with little to do
 };
 
 // Units are counted the same way by the pass and the merge.
@@ -63,11 +63,17 @@ __device__ __forceinline__ int units_of(const TreeParams& a, int b) {
   return s.steps * s.tiles * a.kv.num_kv_heads;
 }
 
+// As many ranges as the chip holds workgroups, or `few` (one to a compute unit) where those would have fewer than eight units each: a range costs a
+// partial result of RT rows that is written and read back, and a second workgroup on the compute unit gains less than that.  Two / one to a
+// compute unit: one request of 8000 tokens with 26 nodes 42 / 33 us, 4 of 2100 38 / 32, with 60 nodes 48 / 40, 8 of 2100 46 / 39; 16 of 4000
+// (16 units each) 78 / 79, 32 of 4096 with 32 nodes 118 / 130.
+constexpr int kFewUnits = 8;
+
 // Range w of n has units range_begin(w) .. range_begin(w + 1) - 1.
 struct Ranges {
   int n, each, longer;         // the first `longer` ranges have each + 1 units, the others `each`
-  __device__ __forceinline__ Ranges(int total, int workgroups) {
-    n = max(1, min(total, workgroups));
+  __device__ __forceinline__ Ranges(int total, int workgroups, int few) {
+    n = max(1, min(total, total < kFewUnits * workgroups ? few : workgroups));
     each = total / n;
     longer = total - each * n;
   }
@@ -95,7 +101,7 @@ struct Share {
   int b, ub;                   // the request that has unit u0, and that request's first unit
   // units: of a request; each(c): called for every 64 requests; prefix: the first workgroup leaves the units before every request, and all of them, there
   template <typename F, typename Each>
-  __device__ __forceinline__ Share(int batch, int workgroups, int32_t* prefix, F units, Each each) {
+  __device__ __forceinline__ Share(int batch, int workgroups, int few, int32_t* prefix, F units, Each each) {
     const int lane = threadIdx.x & 63;
     int total = 0, mine = 0, upto = 0;
     for (int c = 0; c < batch; c += 64) {
@@ -104,12 +110,12 @@ struct Share {
       total = __builtin_amdgcn_readlane(upto, 63);
       each(c);
     }
-    const Ranges ranges(total, workgroups);
+    const Ranges ranges(total, workgroups, few);
     // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
     w = blockIdx.x;
-    if (ranges.n == workgroups && workgroups % 8 == 0) w = (w & 7) * (workgroups >> 3) + (w >> 3);
     u0 = u1 = b = ub = 0;
     if (w >= ranges.n) return;
+    if (ranges.n % 8 == 0) w = (w & 7) * (ranges.n >> 3) + (w >> 3);
     u0 = ranges.begin(w);
     u1 = ranges.begin(w + 1);
     const bool leaves = prefix && w == 0 && threadIdx.x < 64;
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   uint8_t* const vtile = smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
 
-  const Share share(kv.batch, a.ranges, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
+  const Share share(kv.batch, a.ranges, a.few, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
     // contexts without a token have no unit: their rows are shared out among the workgroups
     for (uint64_t none = __ballot(c + lane < kv.batch && kv.seq_lens[min(c + lane, kv.batch - 1)] <= 0); none; none &= none - 1) {
       const int r = c + __builtin_ctzll(none);
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(128) void tree_merge(TreeParams a) {
   constexpr int kLanes = D / 4, kRows = 128 / kLanes;
   const KvView& kv = a.kv;
   const int lane = threadIdx.x & 63, part = threadIdx.x % kLanes;
-  const Ranges ranges(a.prefix[kv.batch], a.ranges);
+  const Ranges ranges(a.prefix[kv.batch], a.ranges, a.few);
   const int w = blockIdx.x + 1;
   if (w >= ranges.n) return;
   const int u = ranges.begin(w);
@@ -644,7 +650,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % C::WR, wt = wave / C::WR, n = lane & 31, g2 = lane >> 5;
   const float scale2 = kv.sm_scale * kLog2e;
-  const Share share(kv.batch, gridDim.x, nullptr, [&](int r) {
+  const Share share(kv.batch, gridDim.x, gridDim.x, nullptr, [&](int r) {
     const Shape sh = shape_of<TS, RT>(a, r);
     return sh.rows > 0 ? sh.steps * kv.num_kv_heads : 0;
   }, [](int) {});
@@ -770,9 +776,12 @@ TreePlan plan_of(const KvView& kv, int max_nodes, bool f32) {
     p.ts = groups <= 1 ? 128 : 64;
     per_cu = 1;
   } else {
-    p.rt = groups <= 1 ? 32 : groups <= 2 ? 64 : groups <= 4 ? 128 : 256;
+    // 256 rows to a workgroup read K and V once for them, 128 make twice as many units: one request of 2100 tokens with 60 nodes 36 / 30 us, 4 49 / 40,
+    // 128 of 1-8 K tokens 788 / 992
+    const bool many = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * ((rows + 255) / 256) * ((kv.max_seq_len + 63) / 64) >= 8 * static_cast<int64_t>(num_cus());
+    p.rt = groups <= 1 ? 32 : groups <= 2 ? 64 : groups <= 4 || !many ? 128 : 256;
     p.ts = groups <= 1 ? 128 : 64;
-    per_cu = groups <= 4 ? 2 : 1;
+    per_cu = p.rt <= 128 ? 2 : 1;
   }
   p.steps_max = (kv.max_seq_len + p.ts - 1) / p.ts;
   p.tiles = static_cast<int64_t>(kv.batch) * kv.num_kv_heads * ((rows + p.rt - 1) / p.rt);
@@ -898,6 +907,7 @@ hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
   p.part_o = reinterpret_cast<float*>(ws + w.o);
   p.lse2 = t.scores ? reinterpret_cast<float*>(ws + w.lse2) : nullptr;
   p.ranges = plan.ranges;
+  p.few = std::min(plan.ranges, num_cus());
   const bool wide = kv.head_dim == 128;
   if (!f32) {
     if (t.kv_dtype == PILLAR_BF16) return wide ? launch_bf16<128, PILLAR_BF16>(p, plan, t, s) : launch_bf16<64, PILLAR_BF16>(p, plan, t, s);
