@@ -9,11 +9,16 @@
 // disjoint, so all rows move at once, in place, and no fewer could: at five new tokens a step at most five rows of a head move where
 // closing the gaps would move the whole cache.  Positions travel with the rows, as a slot no longer says how old a token is.
 //
-// Two launches:
-//   evict_select  one workgroup per (request, KV head): the weights, a radix select of the K'-th key, the list of holes and sources
-//                 in order, and the moves within weights and positions;
-//   evict_move    the rows of K and V.
+// One or two launches:
+//   evict_select  one workgroup per (request, KV head): the weights, a radix select of the K'-th key, the list of holes and sources in
+//                 order, the moves within weights and positions, and, where the launch fills the chip, the rows of K and V;
+//   evict_move    else, the rows of K and V by workgroups of their own.
+//
+// A step at the budget moves a few rows: it is as long as a chain of loads (lengths, state, page ids, rows), two histograms and their
+// barriers.  So the keys stay in registers from one load on, and a digit of the K'-th key that all its keys survive ends the search (the
+// second of three, unless weights agree in 22 bits).
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "page_scale.hpp"
@@ -21,8 +26,8 @@
 namespace pillar {
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kMoveThreads = 256;
+constexpr int kMoveList = 1024;          // moves whose list is kept in LDS
 constexpr uint32_t kProtected = 0xffffffffu;
 
 struct MoveWs {
@@ -41,259 +46,404 @@ __device__ __forceinline__ float accumulate(float weight, float decay, float sco
   return weight * decay + score;
 }
 
-__global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, MoveWs ws) {
-  __shared__ uint32_t hist[2048];
-  __shared__ uint32_t s_scan[2][kSelWaves];
-  __shared__ int s_last[kSelWaves];
-  __shared__ uint32_t s_digit, s_above;
-  const KvView& kv = a.kv;
-  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t pair = static_cast<int64_t>(b) * kv.num_kv_heads + g;
-  const int len = min(max(kv.seq_lens[b], 0), kv.max_seq_len);
-  const int old = min(max(a.old_lens[b], 0), len), keep = min(max(a.budgets[b], 0), len);
-  float* weights = a.weights + pair * a.state_stride;
-  int32_t* positions = a.positions + pair * a.state_stride;
-  const float* scores = a.scores ? a.scores + pair * a.score_stride : nullptr;
-
-  // ---- the newest position so far ----
-  int last = -1;
-  for (int t = tid; t < old; t += kSelThreads) last = max(last, positions[t]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) last = max(last, __shfl_xor(last, o, 64));
-  if (lane == 0) s_last[wave] = last;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kSelWaves; ++i) last = max(last, s_last[i]);
-  const int64_t recent_from = static_cast<int64_t>(last) + (len - old) - a.recent_tokens;      // positions beyond it are protected
-
-  auto weight_of = [&](int t) {
-    const float s = scores ? scores[t] : 0.f;
-    if (t >= old) return s;
-    return scores ? accumulate(weights[t], a.decay, s) : weights[t];
-  };
-  auto position_of = [&](int t) { return t < old ? positions[t] : last + 1 + (t - old); };
-  auto key_of = [&](int t) {
-    const int pos = position_of(t);
-    return pos < a.sink_tokens || pos > recent_from ? kProtected : weight_key(weight_of(t));
-  };
-
-  // ---- the K'-th largest key, by digits of 11, 11 and 10 bits; `need`: how many of the keys equal to it stay ----
-  uint32_t kth = 0, need = 0, equal = 0;
-  if (keep > 0 && keep < len) {
-    uint32_t prefix = 0, want = keep;
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-      for (int i = tid; i < bins; i += kSelThreads) hist[i] = 0;
-      __syncthreads();
-      for (int t = tid; t < len; t += kSelThreads) {
-        const uint32_t k = key_of(t);
-        if (pass == 0 || (k >> (shift + (pass == 1 ? 11 : 10))) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-      }
-      __syncthreads();
-      // from the top: each thread has `per` bins; the digit is where the running count reaches `want`
-      const int per = bins / kSelThreads;
-      uint32_t mine = 0;
-      for (int i = 0; i < per; ++i) mine += hist[bins - 1 - (tid * per + i)];
-      uint32_t upto = mine;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += x;
-      }
-      if (lane == 63) s_scan[0][wave] = upto;
-      __syncthreads();
-      for (int i = 0; i < wave; ++i) upto += s_scan[0][i];
-      if (upto >= want && upto - mine < want) {
-        uint32_t above = upto - mine;
-        for (int i = 0; i < per; ++i) {
-          const int bin = bins - 1 - (tid * per + i);
-          if (above + hist[bin] >= want) {
-            s_digit = bin;
-            s_above = above;
-            break;
-          }
-          above += hist[bin];
-        }
-      }
-      __syncthreads();
-      prefix = prefix << (pass == 2 ? 10 : 11) | s_digit;
-      equal = hist[s_digit];
-      want -= s_above;
-      __syncthreads();
-    }
-    kth = prefix;
-    need = want;
-  } else if (keep == len) {
-    need = equal = 0x7fffffffu;                          // everything stays: every key is >= 0
-  } else {
-    kth = kProtected;                                    // nothing does
-  }
-  const bool ties = need < equal;
-
-  // ---- in order of the slots: weights and positions of what stays, and the list of holes and sources ----
-  int32_t* list = ws.list + pair * kv.max_seq_len;
-  uint32_t base_eq = 0, base_move = 0, holes = 0;
-  for (int t0 = 0; t0 < len; t0 += kSelThreads) {
-    const int t = t0 + tid;
-    const bool there = t < len;
-    const uint32_t k = there ? key_of(t) : 0;
-    bool stays = there && (keep == len || k > kth);
-    const bool eq = there && keep < len && k == kth;
-    if (ties) {
-      const uint64_t bits = __ballot(eq);
-      if (lane == 0) s_scan[0][wave] = __popcll(bits);
-      __syncthreads();
-      uint32_t before = base_eq, all = 0;
-      for (int i = 0; i < kSelWaves; ++i) {
-        before += i < wave ? s_scan[0][i] : 0;
-        all += s_scan[0][i];
-      }
-      stays |= eq && before + __popcll(bits & ((1ull << lane) - 1)) < need;
-      base_eq += all;
-    } else {
-      stays |= eq && need > 0;
-    }
-    const bool moves = there && (t < keep ? !stays : stays);
-    const uint64_t bits = __ballot(moves);
-    if (lane == 0) s_scan[1][wave] = __popcll(bits);
-    __syncthreads();
-    uint32_t before = base_move, all = 0;
-    for (int i = 0; i < kSelWaves; ++i) {
-      before += i < wave ? s_scan[1][i] : 0;
-      all += s_scan[1][i];
-    }
-    if (moves) list[before + __popcll(bits & ((1ull << lane) - 1))] = t;
-    base_move += all;
-    if (t < keep && stays) {
-      if (t >= old || scores) weights[t] = weight_of(t);
-      if (t >= old) positions[t] = position_of(t);
-    }
-    __syncthreads();
-  }
-  holes = base_move / 2;                                 // as many sources as holes, and all holes come first
-  // (weights and positions beyond K' are as they were, the list is complete: the barriers above)
-  for (uint32_t i = tid; i < holes; i += kSelThreads) {
-    const int from = list[holes + i], to = list[i];
-    weights[to] = weight_of(from);
-    positions[to] = position_of(from);
-  }
-  if (tid == 0) {
-    ws.moves[pair] = holes;
-    ws.kept[pair] = keep;
-    if (kv.k_scale && holes) {
-      const int64_t at = static_cast<int64_t>(kv.block_table[static_cast<int64_t>(b) * kv.block_table_stride + (keep >> kv.page_shift)]) * kv.num_kv_heads + g;
-      ws.edge[2 * pair] = kv.k_scale[at];
-      ws.edge[2 * pair + 1] = kv.v_scale[at];
-    }
-  }
+// running sum over the lanes of a wavefront
+__device__ __forceinline__ int lanes_inclusive(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);    // row_bcast 15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // row_bcast 31
+  return v;
 }
 
-// ---- rows of 16-byte pieces, copied ----
-__global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a, MoveWs ws, int esz) {
-  const KvView& kv = a.kv;
-  const int g = blockIdx.y, b = blockIdx.z;
-  const int64_t pair = static_cast<int64_t>(b) * kv.num_kv_heads + g;
-  if (g == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.new_lens[b] = ws.kept[pair];
-  const int moves = ws.moves[pair];
-  const int32_t* list = ws.list + pair * kv.max_seq_len;
-  const RowPlace at(kv, b, g, esz);
-  const int pieces = kv.head_dim * esz / 16, shift = __builtin_ctz(pieces), rows = kMoveThreads >> shift;
-  const int piece = 16 * (threadIdx.x & (pieces - 1));
+// ---- rows of K and V into the holes: worker `me` of `workers` threads (fp8: wavefronts) ----
+template <typename Hole, typename Source>
+__device__ __forceinline__ void copy_rows(const RowPlace& at, int pieces, int moves, Hole hole, Source source, int me, int workers) {
+  const int shift = __builtin_ctz(pieces), piece = 16 * (me & (pieces - 1));
 #pragma unroll 2
-  for (int i = blockIdx.x * rows + (threadIdx.x >> shift); i < moves; i += gridDim.x * rows) {
-    const int64_t from = at.at(list[moves + i]) + piece, to = at.at(list[i]) + piece;
+  for (int i = me >> shift; i < moves; i += workers >> shift) {
+    const int64_t from = at.at(source(i)) + piece, to = at.at(hole(i)) + piece;
     const u32x4 k = *reinterpret_cast<const u32x4*>(at.k + from), v = *reinterpret_cast<const u32x4*>(at.v + from);
     *reinterpret_cast<u32x4*>(at.k + to) = k;
     *reinterpret_cast<u32x4*>(at.v + to) = v;
   }
 }
 
-// ---- fp8: a wavefront per page that has holes ----
-__global__ __launch_bounds__(kMoveThreads) void evict_move_fp8(EvictArgs a, MoveWs ws) {
-  const KvView& kv = a.kv;
-  const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
-  const int64_t pair = static_cast<int64_t>(b) * kv.num_kv_heads + g;
-  const int keep = ws.kept[pair], moves = ws.moves[pair];
-  if (g == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.new_lens[b] = keep;
-  if (moves == 0) return;
-  const int32_t* holes = ws.list + pair * kv.max_seq_len;
-  const int32_t* sources = holes + moves;
-  const RowPlace at(kv, b, g, 1);
+// fp8: a wavefront per page that has holes (ascending), as its scale is a matter of all its rows
+template <typename Hole, typename Source>
+__device__ __forceinline__ void recode_pages(const KvView& kv, const RowPlace& at, int g, int keep, const float (&edge_scale)[2], int moves, Hole hole, Source source,
+                                             int me, int workers) {
+  const int lane = threadIdx.x & 63;
   float* k_scale = const_cast<float*>(kv.k_scale) + g;
   float* v_scale = const_cast<float*>(kv.v_scale) + g;
   const int pieces = kv.head_dim / 16, shift = __builtin_ctz(pieces), rows = 64 >> shift;
   const int piece = 16 * (lane & (pieces - 1));
-  const int edge = keep >> at.shift;                     // the one page that may have rows of both kinds: its scales are read from the workspace
+  const int edge = keep >> at.shift;                     // the one page that may have rows of both kinds: its scales are those it had
   auto scales_of = [&](int t, float& ks, float& vs) {
     if ((t >> at.shift) == edge) {
-      ks = ws.edge[2 * pair];
-      vs = ws.edge[2 * pair + 1];
+      ks = edge_scale[0];
+      vs = edge_scale[1];
     } else {
       const int64_t s = static_cast<int64_t>(at.page(t)) * kv.num_kv_heads;
       ks = k_scale[s];
       vs = v_scale[s];
     }
   };
-  auto hole_at_or_after = [&](int t) {
-    int lo = 0, hi = moves;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (holes[mid] < t) lo = mid + 1;
-      else hi = mid;
-    }
-    return lo;
-  };
-  const int pages = (keep + at.mask) >> at.shift, waves = kMoveThreads / 64;
-  for (int p = blockIdx.x * waves + (threadIdx.x >> 6); p < pages; p += gridDim.x * waves) {
-    const int t0 = p << at.shift, live = min(at.mask + 1, keep - t0);
-    const int h0 = hole_at_or_after(t0), h1 = hole_at_or_after(t0 + live);
-    if (h0 == h1) continue;
-    const int page = at.page(t0);
-    float kn = 0.f, vn = 0.f;
-    for (int h = h0 + lane; h < h1; h += 64) {
-      float ks, vs;
-      scales_of(sources[h], ks, vs);
-      kn = fmaxf(kn, ks);
-      vn = fmaxf(vn, vs);
-    }
+  for (int c = 64 * me; c < moves; c += 64 * workers) {
+    const bool first = c + lane < moves && (c + lane == 0 || hole(c + lane) >> at.shift != hole(c + lane - 1) >> at.shift);
+    for (uint64_t left = __ballot(first); left; left &= left - 1) {
+      const int h0 = c + __builtin_ctzll(left), t0 = hole(h0) & ~at.mask, live = min(at.mask + 1, keep - t0);
+      int h1 = h0 + 1;                                   // past the page's last hole
+      for (int ahead = 0;; ahead += 64) {
+        const int h = h0 + 1 + ahead + lane;
+        const uint64_t out = __ballot(h >= moves || hole(min(h, moves - 1)) - t0 >= live);
+        if (out) {
+          h1 += ahead + __builtin_ctzll(out);
+          break;
+        }
+      }
+      const int page = at.page(t0);
+      float kn = 0.f, vn = 0.f;
+      for (int h = h0 + lane; h < h1; h += 64) {
+        float ks, vs;
+        scales_of(source(h), ks, vs);
+        kn = fmaxf(kn, ks);
+        vn = fmaxf(vn, vs);
+      }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      kn = fmaxf(kn, __shfl_xor(kn, o, 64));
-      vn = fmaxf(vn, __shfl_xor(vn, o, 64));
+      for (int o = 32; o > 0; o >>= 1) {
+        kn = fmaxf(kn, __shfl_xor(kn, o, 64));
+        vn = fmaxf(vn, __shfl_xor(vn, o, 64));
+      }
+      const float ko = k_scale[static_cast<int64_t>(page) * kv.num_kv_heads], vo = v_scale[static_cast<int64_t>(page) * kv.num_kv_heads];
+      if (h1 - h0 < live) {                              // some rows stay
+        kn = fmaxf(kn, ko);
+        vn = fmaxf(vn, vo);
+        const float kr = scale_ratio(ko, kn), vr = scale_ratio(vo, vn);
+        if (kr != 1.f || vr != 1.f) {
+          int h = h0;                                    // the next hole, as the rows go by
+          for (int r0 = 0; r0 < live; r0 += rows) {
+            uint32_t gone = 0;                           // rows of this turn that are holes
+            for (; h < h1 && hole(h) - t0 < r0 + rows; ++h) gone |= 1u << (hole(h) - t0 - r0);
+            const int r = lane >> shift;
+            if (r0 + r >= live || (gone >> r & 1u)) continue;
+            const int64_t to = at.at(page, t0 + r0 + r) + piece;
+            u32x4* kp = reinterpret_cast<u32x4*>(at.k + to);
+            u32x4* vp = reinterpret_cast<u32x4*>(at.v + to);
+            *kp = rescale_codes(*kp, kr);
+            *vp = rescale_codes(*vp, vr);
+          }
+        }
+      }
+      for (int h = h0 + (lane >> shift); h < h1; h += rows) {
+        const int from = source(h);
+        float ks, vs;
+        scales_of(from, ks, vs);
+        const int64_t src = at.at(from) + piece, to = at.at(page, hole(h)) + piece;
+        const u32x4 k = *reinterpret_cast<const u32x4*>(at.k + src), v = *reinterpret_cast<const u32x4*>(at.v + src);
+        *reinterpret_cast<u32x4*>(at.k + to) = rescale_codes(k, scale_ratio(ks, kn));
+        *reinterpret_cast<u32x4*>(at.v + to) = rescale_codes(v, scale_ratio(vs, vn));
+      }
+      // (the whole wavefront has read the old scale)
+      if (lane == 0) {
+        k_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = kn;
+        v_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = vn;
+      }
     }
-    const float ko = k_scale[static_cast<int64_t>(page) * kv.num_kv_heads], vo = v_scale[static_cast<int64_t>(page) * kv.num_kv_heads];
-    if (h1 - h0 < live) {                                // some rows stay
-      kn = fmaxf(kn, ko);
-      vn = fmaxf(vn, vo);
-      const float kr = scale_ratio(ko, kn), vr = scale_ratio(vo, vn);
-      if (kr != 1.f || vr != 1.f) {
-        for (int i = lane >> shift; i < live; i += rows) {
-          bool hole = false;
-          const int at_or_after = hole_at_or_after(t0 + i);
-          if (at_or_after < h1) hole = holes[at_or_after] == t0 + i;
-          if (hole) continue;
-          const int64_t to = at.at(page, t0 + i) + piece;
-          u32x4* kp = reinterpret_cast<u32x4*>(at.k + to);
-          u32x4* vp = reinterpret_cast<u32x4*>(at.v + to);
-          *kp = rescale_codes(*kp, kr);
-          *vp = rescale_codes(*vp, vr);
+  }
+}
+
+// THREADS: a thread has NQ times four neighbouring tokens in registers.  MANY: rows longer than that are walked in blocks, their keys worked
+// out anew each time.
+template <int THREADS, int NQ, bool MANY>
+__global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a, MoveWs ws, int esz, bool wide, bool moves_rows) {
+  constexpr int kWaves = THREADS / 64, kSpan = 4 * THREADS, kBlock = NQ * kSpan;
+  constexpr bool kHold = NQ <= 2;        // weights and positions stay in registers beside the keys
+  static_assert(NQ * kWaves <= 128, "");
+  __shared__ uint32_t hist[3][2048];
+  __shared__ int s_tot[2][NQ * kWaves];
+  __shared__ uint32_t s_sum[kWaves];
+  __shared__ int s_last[kWaves];
+  __shared__ uint32_t s_digit[3], s_above[3];
+  __shared__ int s_hole[kMoveList], s_from[kMoveList], s_pos[kMoveList];
+  __shared__ float s_w[kMoveList];
+  const KvView& kv = a.kv;
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t pair = static_cast<int64_t>(b) * kv.num_kv_heads + g;
+  const int len = min(max(kv.seq_lens[b], 0), kv.max_seq_len);
+  const int old = min(max(a.old_lens[b], 0), len), keep = min(max(a.budgets[b], 0), len);
+  float* weights = a.weights + pair * a.state_stride;
+  int32_t* positions = a.positions + pair * a.state_stride;
+  const float* scores = a.scores ? a.scores + pair * a.score_stride : nullptr;
+  for (int i = tid; i < 3 * 2048; i += THREADS) (&hist[0][0])[i] = 0;
+
+  auto read4 = [&](const auto* p, int t, auto (&x)[4]) { // p[t .. t+3], those that are tokens
+    typedef std::remove_reference_t<decltype(x[0])> T;
+    typedef T vec __attribute__((ext_vector_type(4)));
+    if (wide && t + 4 <= len) {
+      const vec y = *reinterpret_cast<const vec*>(p + t);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = y[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = t + j < len ? p[t + j] : T(0);
+    }
+  };
+  auto first_of = [&](int block, int q) { return block * kBlock + q * kSpan + 4 * tid; };
+  auto weights_at = [&](int t, float (&w)[4]) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (scores) read4(scores, t, s);
+    if (t < old) {
+      read4(weights, t, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = t + j >= old ? s[j] : scores ? accumulate(w[j], a.decay, s[j]) : w[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = s[j];
+    }
+  };
+  const int blocks = MANY ? (len + kBlock - 1) / kBlock : 1;
+
+  // ---- what is there, and the newest position so far ----
+  float w[kHold ? NQ : 1][4];
+  int pos[kHold ? NQ : 1][4];
+  int last = -1;
+  for (int block = 0; block < blocks; ++block) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int t = first_of(block, q), at = kHold ? q : 0;
+      if (kHold) weights_at(t, w[at]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) pos[at][j] = -1;
+      if (t < old) {
+        read4(positions, t, pos[at]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) last = t + j < old ? max(last, pos[at][j]) : last;
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) last = max(last, __shfl_xor(last, o, 64));
+  if (lane == 0) s_last[wave] = last;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) last = max(last, s_last[i]);
+  const int64_t recent_from = static_cast<int64_t>(last) + (len - old) - a.recent_tokens;      // positions beyond it are protected
+  auto numbered = [&](int t, int p) { return t < old ? p : last + 1 + (t - old); };
+  auto key_of = [&](int p, float weight) { return p < a.sink_tokens || p > recent_from ? kProtected : weight_key(weight); };
+
+  uint32_t key[NQ][4];
+  auto load_keys = [&](int block) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int t = first_of(block, q), at = kHold ? q : 0;
+      if (!kHold || MANY) {
+        weights_at(t, w[at]);
+        if (t < old) read4(positions, t, pos[at]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) key[q][j] = key_of(numbered(t + j, pos[at][j]), w[at][j]);
+    }
+  };
+  load_keys(0);
+
+  // ---- the K'-th largest key, from the top: 11, 11 and 10 bits ----
+  int shift = 32;
+  uint32_t prefix = 0, want = keep, equal = 0;           // keys whose bits from `shift` on are `prefix`: `equal` of them, `want` stay
+  if (keep > 0 && keep < len) {
+    for (int pass = 0; pass < 3; ++pass) {
+      const int bits = pass == 2 ? 10 : 11, above_shift = shift;
+      const uint32_t bins = 1u << bits;
+      shift -= bits;
+      for (int block = 0; block < blocks; ++block) {
+        if (MANY && (pass > 0 || block > 0)) load_keys(block);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (first_of(block, q) + j < len && (pass == 0 || key[q][j] >> above_shift == prefix)) atomicAdd(&hist[pass][key[q][j] >> shift & (bins - 1)], 1u);
+      }
+      __syncthreads();
+      constexpr int kMost = 2048 / THREADS;              // bins of a thread, from the top
+      const int per = pass == 2 ? (kMost + 1) / 2 : kMost;
+      int mine = 0;
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        const int bin = static_cast<int>(bins) - 1 - (tid * per + i);
+        if (i < per && bin >= 0) mine += hist[pass][bin];
+      }
+      int upto = lanes_inclusive(mine);
+      if (lane == 63) s_sum[wave] = upto;
+      __syncthreads();
+      for (int i = 0; i < wave; ++i) upto += s_sum[i];
+      if (upto >= static_cast<int>(want) && upto - mine < static_cast<int>(want)) {
+        uint32_t above = upto - mine;
+        for (int i = 0; i < per; ++i) {
+          const int bin = static_cast<int>(bins) - 1 - (tid * per + i);
+          if (above + hist[pass][bin] >= want) {
+            s_digit[pass] = bin;
+            s_above[pass] = above;
+            break;
+          }
+          above += hist[pass][bin];
+        }
+      }
+      __syncthreads();
+      prefix = prefix << bits | s_digit[pass];
+      equal = hist[pass][s_digit[pass]];
+      want -= s_above[pass];
+      if (want == equal) break;
+    }
+  }
+  const bool ties = want < equal;                        // (all bits told apart)
+  auto stays_of = [&](uint32_t k) { return keep == len || (keep > 0 && (k >> shift > prefix || (k >> shift == prefix && !ties))); };
+  auto ties_of = [&](uint32_t k) { return ties && k >> shift == prefix; };
+
+  // ---- in order of the slots: ranks of flagged tokens ----
+  // flags[q]: four bits; rank[q]: flagged tokens before this thread's of quad q, in this block and `base` before; returns base and all of the block
+  auto ranks = [&](const uint32_t (&flags)[NQ], int (&rank)[NQ], int base, int* totals) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int mine = __popc(flags[q]), upto = lanes_inclusive(mine);
+      if (lane == 63) totals[q * kWaves + wave] = upto;
+      rank[q] = upto - mine;
+    }
+    __syncthreads();
+    int x0 = lane < NQ * kWaves ? totals[lane] : 0, x1 = 64 + lane < NQ * kWaves ? totals[64 + lane] : 0;
+    const int i0 = lanes_inclusive(x0), half = __builtin_amdgcn_readlane(i0, 63), i1 = lanes_inclusive(x1) + half;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int e = q * kWaves + wave;
+      rank[q] += base + (e < 64 ? __builtin_amdgcn_readlane(i0 - x0, e & 63) : __builtin_amdgcn_readlane(i1 - x1, e & 63));
+    }
+    return base + __builtin_amdgcn_readlane(i1, 63);
+  };
+
+  int32_t* list = ws.list + pair * kv.max_seq_len;
+  int ties_before = 0, flagged = 0;
+  for (int block = 0; block < blocks; ++block) {
+    if (MANY) load_keys(block);
+    uint32_t stays[NQ], moves[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      stays[q] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) stays[q] |= static_cast<uint32_t>(first_of(block, q) + j < len && stays_of(key[q][j])) << j;
+    }
+    if (ties) {
+      uint32_t equals[NQ];
+      int rank[NQ];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        equals[q] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) equals[q] |= static_cast<uint32_t>(first_of(block, q) + j < len && ties_of(key[q][j])) << j;
+      }
+      ties_before = ranks(equals, rank, ties_before, s_tot[0]);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (equals[q] >> j & 1u) stays[q] |= static_cast<uint32_t>(rank[q] + __popc(equals[q] & ((1u << j) - 1)) < static_cast<int>(want)) << j;
+    }
+    int rank[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      moves[q] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = first_of(block, q) + j;
+        moves[q] |= static_cast<uint32_t>(t < len && (t < keep) != (stays[q] >> j & 1u)) << j;
+      }
+    }
+    flagged = ranks(moves, rank, flagged, s_tot[1]);
+    const int holes = flagged / 2;                       // (of a row in one block: as many sources as holes, all holes first)
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int t0 = first_of(block, q), at = kHold ? q : 0;
+      if (t0 >= len) continue;
+      if (!kHold) {
+        weights_at(t0, w[at]);
+        if (t0 < old) read4(positions, t0, pos[at]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = t0 + j;
+        if (moves[q] >> j & 1u) {
+          const int r = rank[q] + __popc(moves[q] & ((1u << j) - 1));
+          list[r] = t;
+          if (!MANY && t < keep && r < kMoveList) s_hole[r] = t;
+          if (!MANY && t >= keep && r - holes < kMoveList) {
+            s_from[r - holes] = t;
+            s_w[r - holes] = w[at][j];
+            s_pos[r - holes] = numbered(t, pos[at][j]);
+          }
+        } else if (t < keep) {
+          if (t >= old || scores) weights[t] = w[at][j];
+          if (t >= old) positions[t] = numbered(t, pos[at][j]);
         }
       }
     }
-    for (int h = h0 + (lane >> shift); h < h1; h += rows) {
-      const int from = sources[h];
-      float ks, vs;
-      scales_of(from, ks, vs);
-      const int64_t src = at.at(from) + piece, to = at.at(page, holes[h]) + piece;
-      const u32x4 k = *reinterpret_cast<const u32x4*>(at.k + src), v = *reinterpret_cast<const u32x4*>(at.v + src);
-      *reinterpret_cast<u32x4*>(at.k + to) = rescale_codes(k, scale_ratio(ks, kn));
-      *reinterpret_cast<u32x4*>(at.v + to) = rescale_codes(v, scale_ratio(vs, vn));
+    if (MANY) __syncthreads();                           // (s_tot is written again)
+  }
+  __syncthreads();                                       // the list is complete; weights and positions beyond K' are as they were
+  const int holes = flagged / 2;
+  auto hole = [&](int i) { return !MANY && i < kMoveList ? s_hole[i] : list[i]; };
+  auto source = [&](int i) { return !MANY && i < kMoveList ? s_from[i] : list[holes + i]; };
+  for (int i = tid; i < holes; i += THREADS) {
+    const int to = hole(i);
+    if (!MANY && i < kMoveList) {
+      weights[to] = s_w[i];
+      positions[to] = s_pos[i];
+    } else {
+      const int t = list[holes + i];
+      const float s = scores ? scores[t] : 0.f;
+      weights[to] = t >= old ? s : scores ? accumulate(weights[t], a.decay, s) : weights[t];
+      positions[to] = numbered(t, positions[t]);
     }
-    // (every lane has read the old scale: the reads above are in program order for the whole wavefront)
-    if (lane == 0) {
-      k_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = kn;
-      v_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = vn;
+  }
+  float edge[2] = {0.f, 0.f};
+  if (esz == 1 && holes) {
+    const int64_t at = static_cast<int64_t>(kv.block_table[static_cast<int64_t>(b) * kv.block_table_stride + (keep >> kv.page_shift)]) * kv.num_kv_heads + g;
+    edge[0] = kv.k_scale[at];
+    edge[1] = kv.v_scale[at];
+  }
+  if (!moves_rows) {
+    if (tid == 0) {
+      ws.moves[pair] = holes;
+      ws.kept[pair] = keep;
+      ws.edge[2 * pair] = edge[0];
+      ws.edge[2 * pair + 1] = edge[1];
     }
+    return;
+  }
+  if (g == 0 && tid == 0) a.new_lens[b] = keep;
+  const RowPlace at(kv, b, g, esz);
+  if (esz == 1) {
+    __syncthreads();                                     // all have read the scales of the page at K'
+    recode_pages(kv, at, g, keep, edge, holes, hole, source, wave, kWaves);
+  } else {
+    copy_rows(at, kv.head_dim * esz / 16, holes, hole, source, tid, THREADS);
+  }
+}
+
+__global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a, MoveWs ws, int esz) {
+  const KvView& kv = a.kv;
+  const int g = blockIdx.y, b = blockIdx.z;
+  const int64_t pair = static_cast<int64_t>(b) * kv.num_kv_heads + g;
+  const int keep = ws.kept[pair], moves = ws.moves[pair];
+  if (g == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.new_lens[b] = keep;
+  const int32_t* list = ws.list + pair * kv.max_seq_len;
+  auto hole = [&](int i) { return list[i]; };
+  auto source = [&](int i) { return list[moves + i]; };
+  const RowPlace at(kv, b, g, esz);
+  const int me = blockIdx.x * kMoveThreads + threadIdx.x, workers = gridDim.x * kMoveThreads;
+  if (esz == 1) {
+    const float edge[2] = {ws.edge[2 * pair], ws.edge[2 * pair + 1]};
+    recode_pages(kv, at, g, keep, edge, moves, hole, source, me >> 6, workers >> 6);
+  } else {
+    copy_rows(at, kv.head_dim * esz / 16, moves, hole, source, me, workers);
   }
 }
 
@@ -322,19 +472,30 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   ws.kept = reinterpret_cast<int32_t*>(p + w.kept);
   ws.edge = reinterpret_cast<float*>(p + w.edge);
   ws.list = reinterpret_cast<int32_t*>(p + w.list);
+  const int pairs = a.kv.batch * a.kv.num_kv_heads, esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
+  const bool wide = a.state_stride % 4 == 0 && (!a.scores || a.score_stride % 4 == 0) &&
+                    ((reinterpret_cast<uintptr_t>(a.weights) | reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.scores)) & 15u) == 0;
+  // Where there is a workgroup for every compute unit it moves its rows too: a launch less.  (Not where the new lengths replace what the
+  // workgroups of other heads read.)
+  auto apart = [&](const int32_t* p) { return a.new_lens + a.kv.batch <= p || p + a.kv.batch <= a.new_lens; };
+  const bool moves_rows = pairs >= num_cus() && apart(a.kv.seq_lens) && apart(a.old_lens) && apart(a.budgets);
   {
     KernelTimer timer("evict_select", s);
-    hipLaunchKernelGGL(evict_select, dim3(a.kv.num_kv_heads, a.kv.batch), dim3(kSelThreads), 0, s, a, ws);
+    const dim3 grid(a.kv.num_kv_heads, a.kv.batch);
+    const int n = a.kv.max_seq_len;
+    if (n <= 1024) hipLaunchKernelGGL((evict_select<256, 1, false>), grid, dim3(256), 0, s, a, ws, esz, wide, moves_rows);
+    else if (n <= 4096) hipLaunchKernelGGL((evict_select<1024, 1, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
+    else if (n <= 8192) hipLaunchKernelGGL((evict_select<1024, 2, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
+    else if (n <= 32768) hipLaunchKernelGGL((evict_select<1024, 8, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
+    else hipLaunchKernelGGL((evict_select<1024, 8, true>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
   }
-  KernelTimer timer("evict_move", s);
-  const int pairs = a.kv.batch * a.kv.num_kv_heads, esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
-  // at most half of the rows move; as many workgroups as that gives work, and no more than eight per compute unit
-  const int most = a.kv_dtype == PILLAR_FP8_E4M3 ? ((a.kv.max_seq_len + a.kv.page_size - 1) / a.kv.page_size + 3) / 4
-                                                 : (a.kv.max_seq_len / 2 + 15) / 16;
-  const int blocks = std::max(1, std::min(most, (8 * num_cus() + pairs - 1) / pairs));
-  const dim3 grid(blocks, a.kv.num_kv_heads, a.kv.batch);
-  if (a.kv_dtype == PILLAR_FP8_E4M3) hipLaunchKernelGGL(evict_move_fp8, grid, dim3(kMoveThreads), 0, s, a, ws);
-  else hipLaunchKernelGGL(evict_move, grid, dim3(kMoveThreads), 0, s, a, ws, esz);
+  if (!moves_rows) {
+    KernelTimer timer("evict_move", s);
+    // at most half of the rows move; as many workgroups as that gives work, and no more than eight per compute unit
+    const int most = (a.kv.max_seq_len / 2 + 15) / 16;
+    const int blocks = std::max(1, std::min(most, (8 * num_cus() + pairs - 1) / pairs));
+    hipLaunchKernelGGL(evict_move, dim3(blocks, a.kv.num_kv_heads, a.kv.batch), dim3(kMoveThreads), 0, s, a, ws, esz);
+  }
   return hipGetLastError();
 }
 
