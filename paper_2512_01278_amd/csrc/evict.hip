@@ -57,107 +57,167 @@ __device__ __forceinline__ int lanes_inclusive(int v) {
   return v;
 }
 
+// Rows are read several at a time before any is written: the compiler cannot know that no load depends on a store before it.
+constexpr int kBatch = 2;
+
 // ---- rows of K and V into the holes: worker `me` of `workers` threads (fp8: wavefronts) ----
 template <typename Hole, typename Source>
 __device__ __forceinline__ void copy_rows(const RowPlace& at, int pieces, int moves, Hole hole, Source source, int me, int workers) {
-  const int shift = __builtin_ctz(pieces), piece = 16 * (me & (pieces - 1));
-#pragma unroll 2
-  for (int i = me >> shift; i < moves; i += workers >> shift) {
-    const int64_t from = at.at(source(i)) + piece, to = at.at(hole(i)) + piece;
-    const u32x4 k = *reinterpret_cast<const u32x4*>(at.k + from), v = *reinterpret_cast<const u32x4*>(at.v + from);
-    *reinterpret_cast<u32x4*>(at.k + to) = k;
-    *reinterpret_cast<u32x4*>(at.v + to) = v;
+  const int shift = __builtin_ctz(pieces), piece = 16 * (me & (pieces - 1)), step = workers >> shift;
+  for (int i = me >> shift; i < moves; i += kBatch * step) {
+    u32x4 k[kBatch], v[kBatch];
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (i + n * step >= moves) break;
+      const int64_t from = at.at(source(i + n * step)) + piece;
+      k[n] = *reinterpret_cast<const u32x4*>(at.k + from);
+      v[n] = *reinterpret_cast<const u32x4*>(at.v + from);
+    }
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (i + n * step >= moves) break;
+      const int64_t to = at.at(hole(i + n * step)) + piece;
+      *reinterpret_cast<u32x4*>(at.k + to) = k[n];
+      *reinterpret_cast<u32x4*>(at.v + to) = v[n];
+    }
   }
 }
 
-// fp8: a wavefront per page that has holes (ascending), as its scale is a matter of all its rows
+// fp8: LANES lanes take the page that hole h0 is the first one of (holes ascending), as its scale is a matter of all its rows.
+template <int LANES, typename Hole, typename Source>
+__device__ __forceinline__ void recode_page(const KvView& kv, const RowPlace& at, int g, int keep, const float (&edge_scale)[2], int moves, Hole hole, Source source,
+                                            int h0) {
+  const int lane = threadIdx.x & (LANES - 1), mine = threadIdx.x & 63 & ~(LANES - 1);
+  auto vote = [&](bool x) { return __ballot(x) >> mine & (~0ull >> (64 - LANES)); };
+  float* k_scale = const_cast<float*>(kv.k_scale) + g;
+  float* v_scale = const_cast<float*>(kv.v_scale) + g;
+  const int pieces = kv.head_dim / 16, shift = __builtin_ctz(pieces), rows = LANES >> shift;
+  const int piece = 16 * (lane & (pieces - 1)), r = lane >> shift;
+  const int edge = keep >> at.shift;                     // the one page that may have rows of both kinds: its scales are those it had
+  auto scales_of = [&](int t, int page, float& ks, float& vs) {
+    const int64_t s = static_cast<int64_t>(page) * kv.num_kv_heads;
+    const bool there = (t >> at.shift) == edge;
+    ks = there ? edge_scale[0] : k_scale[s];
+    vs = there ? edge_scale[1] : v_scale[s];
+  };
+  const int t0 = hole(h0) & ~at.mask, live = min(at.mask + 1, keep - t0);
+  const int page = at.page(t0);
+  const float ko = k_scale[static_cast<int64_t>(page) * kv.num_kv_heads], vo = v_scale[static_cast<int64_t>(page) * kv.num_kv_heads];
+  int h1 = h0;                                       // past the page's last hole
+  float kn = 0.f, vn = 0.f;
+  for (uint64_t in = ~0ull; in >> (LANES - 1) & 1;) {
+    const int h = h1 + lane;
+    const bool here = h < moves && hole(min(h, moves - 1)) - t0 < live;
+    if (here) {
+      const int from = source(h);
+      float ks, vs;
+      scales_of(from, at.page(from), ks, vs);
+      kn = fmaxf(kn, ks);
+      vn = fmaxf(vn, vs);
+    }
+    in = vote(here);
+    h1 += __popcll(in);
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    kn = fmaxf(kn, __shfl_xor(kn, o, LANES));
+    vn = fmaxf(vn, __shfl_xor(vn, o, LANES));
+  }
+  if (h1 - h0 < live) {                              // some rows stay
+    kn = fmaxf(kn, ko);
+    vn = fmaxf(vn, vo);
+    const float kr = scale_ratio(ko, kn), vr = scale_ratio(vo, vn);
+    auto is_hole = [&](int t) {
+      int lo = h0, hi = h1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (hole(mid) < t) lo = mid + 1;
+        else hi = mid;
+      }
+      return lo < h1 && hole(lo) == t;
+    };
+    if (kr != 1.f || vr != 1.f) {
+      for (int r0 = r; r0 < live; r0 += kBatch * rows) {
+        u32x4 k[kBatch], v[kBatch];
+        uint32_t stay = 0;
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+          const int row = r0 + n * rows;
+          if (row >= live || is_hole(t0 + row)) continue;
+          const int64_t to = at.at(page, t0 + row) + piece;
+          stay |= 1u << n;
+          k[n] = *reinterpret_cast<const u32x4*>(at.k + to);
+          v[n] = *reinterpret_cast<const u32x4*>(at.v + to);
+        }
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+          if (!(stay >> n & 1u)) continue;
+          const int64_t to = at.at(page, t0 + r0 + n * rows) + piece;
+          *reinterpret_cast<u32x4*>(at.k + to) = rescale_codes(k[n], kr);
+          *reinterpret_cast<u32x4*>(at.v + to) = rescale_codes(v[n], vr);
+        }
+      }
+    }
+  }
+  for (int h = h0 + r; h < h1; h += kBatch * rows) {
+    u32x4 k[kBatch], v[kBatch];
+    float kr[kBatch], vr[kBatch];
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (h + n * rows >= h1) break;
+      const int from = source(h + n * rows), src_page = at.page(from);
+      float ks, vs;
+      scales_of(from, src_page, ks, vs);
+      kr[n] = scale_ratio(ks, kn);
+      vr[n] = scale_ratio(vs, vn);
+      const int64_t src = at.at(src_page, from) + piece;
+      k[n] = *reinterpret_cast<const u32x4*>(at.k + src);
+      v[n] = *reinterpret_cast<const u32x4*>(at.v + src);
+    }
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (h + n * rows >= h1) break;
+      const int64_t to = at.at(page, hole(h + n * rows)) + piece;
+      *reinterpret_cast<u32x4*>(at.k + to) = rescale_codes(k[n], kr[n]);
+      *reinterpret_cast<u32x4*>(at.v + to) = rescale_codes(v[n], vr[n]);
+    }
+  }
+  // (all lanes of the page have read its old scale)
+  if (lane == 0) {
+    k_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = kn;
+    v_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = vn;
+  }
+}
+
+// Worker `me` of `workers` wavefronts.  A page is a chain of six loads and little else.  Where there are fewer holes than pages (a step at the budget:
+// a few rows in as many pages) the holes are dealt out, a wavefront to each, which has a page of 16 rows in one turn; else the
+// pages, sixteen lanes to each, four chains side by side.  64 requests, budget 4096, five new tokens: holes to 16 lanes 67 us, to wavefronts
+// 35; 32 prompts of 8 K: pages to wavefronts 110, to 16 lanes 95.
 template <typename Hole, typename Source>
 __device__ __forceinline__ void recode_pages(const KvView& kv, const RowPlace& at, int g, int keep, const float (&edge_scale)[2], int moves, Hole hole, Source source,
                                              int me, int workers) {
-  const int lane = threadIdx.x & 63;
-  float* k_scale = const_cast<float*>(kv.k_scale) + g;
-  float* v_scale = const_cast<float*>(kv.v_scale) + g;
-  const int pieces = kv.head_dim / 16, shift = __builtin_ctz(pieces), rows = 64 >> shift;
-  const int piece = 16 * (lane & (pieces - 1));
-  const int edge = keep >> at.shift;                     // the one page that may have rows of both kinds: its scales are those it had
-  auto scales_of = [&](int t, float& ks, float& vs) {
-    if ((t >> at.shift) == edge) {
-      ks = edge_scale[0];
-      vs = edge_scale[1];
-    } else {
-      const int64_t s = static_cast<int64_t>(at.page(t)) * kv.num_kv_heads;
-      ks = k_scale[s];
-      vs = v_scale[s];
+  const int pages = (keep + at.mask) >> at.shift;
+  if (moves < pages) {
+    for (int h = me; h < moves; h += workers)
+      if (h == 0 || hole(h) >> at.shift != hole(h - 1) >> at.shift) recode_page<64>(kv, at, g, keep, edge_scale, moves, hole, source, h);
+    return;
+  }
+  constexpr int kLanes = 16;
+  for (int p = me * (64 / kLanes) + (threadIdx.x & 63) / kLanes; p < pages; p += workers * (64 / kLanes)) {
+    int lo = 0, hi = moves;                              // the page's first hole
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (hole(mid) < p << at.shift) lo = mid + 1;
+      else hi = mid;
     }
-  };
-  for (int c = 64 * me; c < moves; c += 64 * workers) {
-    const bool first = c + lane < moves && (c + lane == 0 || hole(c + lane) >> at.shift != hole(c + lane - 1) >> at.shift);
-    for (uint64_t left = __ballot(first); left; left &= left - 1) {
-      const int h0 = c + __builtin_ctzll(left), t0 = hole(h0) & ~at.mask, live = min(at.mask + 1, keep - t0);
-      int h1 = h0 + 1;                                   // past the page's last hole
-      for (int ahead = 0;; ahead += 64) {
-        const int h = h0 + 1 + ahead + lane;
-        const uint64_t out = __ballot(h >= moves || hole(min(h, moves - 1)) - t0 >= live);
-        if (out) {
-          h1 += ahead + __builtin_ctzll(out);
-          break;
-        }
-      }
-      const int page = at.page(t0);
-      float kn = 0.f, vn = 0.f;
-      for (int h = h0 + lane; h < h1; h += 64) {
-        float ks, vs;
-        scales_of(source(h), ks, vs);
-        kn = fmaxf(kn, ks);
-        vn = fmaxf(vn, vs);
-      }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        kn = fmaxf(kn, __shfl_xor(kn, o, 64));
-        vn = fmaxf(vn, __shfl_xor(vn, o, 64));
-      }
-      const float ko = k_scale[static_cast<int64_t>(page) * kv.num_kv_heads], vo = v_scale[static_cast<int64_t>(page) * kv.num_kv_heads];
-      if (h1 - h0 < live) {                              // some rows stay
-        kn = fmaxf(kn, ko);
-        vn = fmaxf(vn, vo);
-        const float kr = scale_ratio(ko, kn), vr = scale_ratio(vo, vn);
-        if (kr != 1.f || vr != 1.f) {
-          int h = h0;                                    // the next hole, as the rows go by
-          for (int r0 = 0; r0 < live; r0 += rows) {
-            uint32_t gone = 0;                           // rows of this turn that are holes
-            for (; h < h1 && hole(h) - t0 < r0 + rows; ++h) gone |= 1u << (hole(h) - t0 - r0);
-            const int r = lane >> shift;
-            if (r0 + r >= live || (gone >> r & 1u)) continue;
-            const int64_t to = at.at(page, t0 + r0 + r) + piece;
-            u32x4* kp = reinterpret_cast<u32x4*>(at.k + to);
-            u32x4* vp = reinterpret_cast<u32x4*>(at.v + to);
-            *kp = rescale_codes(*kp, kr);
-            *vp = rescale_codes(*vp, vr);
-          }
-        }
-      }
-      for (int h = h0 + (lane >> shift); h < h1; h += rows) {
-        const int from = source(h);
-        float ks, vs;
-        scales_of(from, ks, vs);
-        const int64_t src = at.at(from) + piece, to = at.at(page, hole(h)) + piece;
-        const u32x4 k = *reinterpret_cast<const u32x4*>(at.k + src), v = *reinterpret_cast<const u32x4*>(at.v + src);
-        *reinterpret_cast<u32x4*>(at.k + to) = rescale_codes(k, scale_ratio(ks, kn));
-        *reinterpret_cast<u32x4*>(at.v + to) = rescale_codes(v, scale_ratio(vs, vn));
-      }
-      // (the whole wavefront has read the old scale)
-      if (lane == 0) {
-        k_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = kn;
-        v_scale[static_cast<int64_t>(page) * kv.num_kv_heads] = vn;
-      }
-    }
+    if (lo < moves && hole(lo) >> at.shift == p) recode_page<kLanes>(kv, at, g, keep, edge_scale, moves, hole, source, lo);
   }
 }
 
 // THREADS: a thread has NQ times four neighbouring tokens in registers.  MANY: rows longer than that are walked in blocks, their keys worked
 // out anew each time.
-template <int THREADS, int NQ, bool MANY>
-__global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a, MoveWs ws, int esz, bool wide, bool moves_rows) {
+template <int THREADS, int NQ, bool MANY, bool FP8>
+__global__ __launch_bounds__(THREADS, THREADS < 1024 ? 1 : NQ <= 2 && !FP8 ? 8 : 4) void evict_select(EvictArgs a, MoveWs ws, int esz, bool wide, bool moves_rows) {
   constexpr int kWaves = THREADS / 64, kSpan = 4 * THREADS, kBlock = NQ * kSpan;
   constexpr bool kHold = NQ <= 2;        // weights and positions stay in registers beside the keys
   static_assert(NQ * kWaves <= 128, "");
@@ -404,7 +464,7 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a, MoveWs ws, 
     }
   }
   float edge[2] = {0.f, 0.f};
-  if (esz == 1 && holes) {
+  if (FP8 && holes) {
     const int64_t at = static_cast<int64_t>(kv.block_table[static_cast<int64_t>(b) * kv.block_table_stride + (keep >> kv.page_shift)]) * kv.num_kv_heads + g;
     edge[0] = kv.k_scale[at];
     edge[1] = kv.v_scale[at];
@@ -420,7 +480,7 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a, MoveWs ws, 
   }
   if (g == 0 && tid == 0) a.new_lens[b] = keep;
   const RowPlace at(kv, b, g, esz);
-  if (esz == 1) {
+  if constexpr (FP8) {
     __syncthreads();                                     // all have read the scales of the page at K'
     recode_pages(kv, at, g, keep, edge, holes, hole, source, wave, kWaves);
   } else {
@@ -428,6 +488,7 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a, MoveWs ws, 
   }
 }
 
+template <bool FP8>
 __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a, MoveWs ws, int esz) {
   const KvView& kv = a.kv;
   const int g = blockIdx.y, b = blockIdx.z;
@@ -439,7 +500,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a, MoveWs w
   auto source = [&](int i) { return list[moves + i]; };
   const RowPlace at(kv, b, g, esz);
   const int me = blockIdx.x * kMoveThreads + threadIdx.x, workers = gridDim.x * kMoveThreads;
-  if (esz == 1) {
+  if constexpr (FP8) {
     const float edge[2] = {ws.edge[2 * pair], ws.edge[2 * pair + 1]};
     recode_pages(kv, at, g, keep, edge, moves, hole, source, me >> 6, workers >> 6);
   } else {
@@ -479,22 +540,31 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   // workgroups of other heads read.)
   auto apart = [&](const int32_t* p) { return a.new_lens + a.kv.batch <= p || p + a.kv.batch <= a.new_lens; };
   const bool moves_rows = pairs >= num_cus() && apart(a.kv.seq_lens) && apart(a.old_lens) && apart(a.budgets);
+  const bool fp8 = a.kv_dtype == PILLAR_FP8_E4M3;
   {
     KernelTimer timer("evict_select", s);
     const dim3 grid(a.kv.num_kv_heads, a.kv.batch);
     const int n = a.kv.max_seq_len;
-    if (n <= 1024) hipLaunchKernelGGL((evict_select<256, 1, false>), grid, dim3(256), 0, s, a, ws, esz, wide, moves_rows);
-    else if (n <= 4096) hipLaunchKernelGGL((evict_select<1024, 1, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
-    else if (n <= 8192) hipLaunchKernelGGL((evict_select<1024, 2, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
-    else if (n <= 32768) hipLaunchKernelGGL((evict_select<1024, 8, false>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
-    else hipLaunchKernelGGL((evict_select<1024, 8, true>), grid, dim3(1024), 0, s, a, ws, esz, wide, moves_rows);
+#define PILLAR_EVICT(threads, quads, many)                                                                                                             \
+  do {                                                                                                                                                 \
+    if (fp8) hipLaunchKernelGGL((evict_select<threads, quads, many, true>), grid, dim3(threads), 0, s, a, ws, esz, wide, moves_rows);                    \
+    else hipLaunchKernelGGL((evict_select<threads, quads, many, false>), grid, dim3(threads), 0, s, a, ws, esz, wide, moves_rows);                       \
+  } while (0)
+    if (n <= 1024) PILLAR_EVICT(256, 1, false);
+    else if (n <= 4096) PILLAR_EVICT(1024, 1, false);
+    else if (n <= 8192) PILLAR_EVICT(1024, 2, false);
+    else if (n <= 32768) PILLAR_EVICT(1024, 8, false);
+    else PILLAR_EVICT(1024, 8, true);
+#undef PILLAR_EVICT
   }
   if (!moves_rows) {
     KernelTimer timer("evict_move", s);
     // at most half of the rows move; as many workgroups as that gives work, and no more than eight per compute unit
     const int most = (a.kv.max_seq_len / 2 + 15) / 16;
     const int blocks = std::max(1, std::min(most, (8 * num_cus() + pairs - 1) / pairs));
-    hipLaunchKernelGGL(evict_move, dim3(blocks, a.kv.num_kv_heads, a.kv.batch), dim3(kMoveThreads), 0, s, a, ws, esz);
+    const dim3 grid(blocks, a.kv.num_kv_heads, a.kv.batch);
+    if (fp8) hipLaunchKernelGGL(evict_move<true>, grid, dim3(kMoveThreads), 0, s, a, ws, esz);
+    else hipLaunchKernelGGL(evict_move<false>, grid, dim3(kMoveThreads), 0, s, a, ws, esz);
   }
   return hipGetLastError();
 }
