@@ -295,13 +295,29 @@ def pillar_extend_indices(indices: torch.Tensor, counts: torch.Tensor, first_new
 _Q_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
+_F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
+
+
+def _refuse(t: torch.Tensor, what: str, wanted: str):
+    raise ValueError(f"{what}: a contiguous {wanted} is wanted, not {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ', strided'}")
+
+
+# The address of a tensor whose type, shape and layout are what the C side takes for granted.  (A tenth of a microsecond per question asked: a
+# whole call takes eight.)
 def _tensor(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
-    """The address of a tensor whose type, shape and layout are what the C side takes for granted."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}"
-                         f"{'' if t.is_contiguous() else ', strided'}")
+        _refuse(t, what, f"{dtype} tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _per_request(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    """int32, one entry per request."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
+        _refuse(t, what, f"int32 tensor of {n}")
     return t.data_ptr()
 
 
@@ -309,9 +325,10 @@ def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, B: int, Hkv: int, max_s
     """Address and stride of [B][Hkv][stride]: rows of at least max_seq_len entries, one behind the other."""
     if t is None:
         return None, 0
-    if t.dtype is not dtype or t.dim() != 3 or t.shape[0] != B or t.shape[1] != Hkv or t.shape[2] < max_seq_len or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor [{B}, {Hkv}, >= {max_seq_len}] is wanted, not {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr(), t.shape[2]
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < max_seq_len or not t.is_contiguous():
+        _refuse(t, what, f"{dtype} tensor [{B}, {Hkv}, >= {max_seq_len}]")
+    return t.data_ptr(), shape[2]
 
 
 def pillar_tree_workspace_bytes(kv: KvCache, max_nodes: int) -> int:
@@ -327,10 +344,10 @@ def pillar_verify_tree(kv: KvCache, q: torch.Tensor, tree_sizes: Optional[torch.
     shape = (B, N, s.num_q_heads, s.head_dim)
     if B != s.batch:
         raise ValueError(f"visible: a row for each of {s.batch} requests is wanted, not {B}")
-    scores_at, stride = _rows(scores, torch.float32, B, s.num_kv_heads, s.max_seq_len, "scores")
-    rc = load().pillar_verify_tree(C.byref(s), _tensor(q, _Q_TORCH[kv.q_dtype], shape, "q"), N, _tensor(tree_sizes, torch.int32, (B,), "tree_sizes"),
-                                   _tensor(visible, torch.int64, (B, N), "visible"), _tensor(out, _Q_TORCH[kv.q_dtype], shape, "out"),
-                                   _tensor(lse, torch.float32, shape[:3], "lse"), scores_at, stride, workspace.data_ptr(),
+    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, "scores")
+    rc = load().pillar_verify_tree(C.byref(s), _tensor(q, _Q_TORCH[kv.q_dtype], shape, "q"), N, _per_request(tree_sizes, B, "tree_sizes"),
+                                   _tensor(visible, _I64, (B, N), "visible"), _tensor(out, _Q_TORCH[kv.q_dtype], shape, "out"),
+                                   _tensor(lse, _F32, shape[:3], "lse"), scores_at, stride, workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(), _stream(stream))
     _check(rc, "pillar_verify_tree")
 
@@ -339,10 +356,10 @@ def pillar_tree_commit(kv: KvCache, tree_sizes: Optional[torch.Tensor], max_node
                        new_lens: torch.Tensor, scores: Optional[torch.Tensor] = None, stream=None) -> None:
     s = kv.c_struct()
     B, M = s.batch, path.shape[-1]
-    scores_at, stride = _rows(scores, torch.float32, B, s.num_kv_heads, s.max_seq_len, "scores")
-    rc = load().pillar_tree_commit(C.byref(s), _tensor(tree_sizes, torch.int32, (B,), "tree_sizes"), max_nodes,
-                                   _tensor(path, torch.int32, (B, M), "path"), _tensor(path_lens, torch.int32, (B,), "path_lens"), M,
-                                   _tensor(new_lens, torch.int32, (B,), "new_lens"), scores_at, stride, _stream(stream))
+    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, "scores")
+    rc = load().pillar_tree_commit(C.byref(s), _per_request(tree_sizes, B, "tree_sizes"), max_nodes,
+                                   _tensor(path, _I32, (B, M), "path"), _per_request(path_lens, B, "path_lens"), M,
+                                   _per_request(new_lens, B, "new_lens"), scores_at, stride, _stream(stream))
     _check(rc, "pillar_tree_commit")
 
 
@@ -356,14 +373,14 @@ def pillar_evict_kv(kv: KvCache, scores: Optional[torch.Tensor], decay: float, o
                     workspace: torch.Tensor, stream=None) -> None:
     s = kv.c_struct()
     B, Hkv, top = s.batch, s.num_kv_heads, s.max_seq_len
-    scores_at, stride = _rows(scores, torch.float32, B, Hkv, top, "scores")
-    weights_at, state_stride = _rows(weights, torch.float32, B, Hkv, top, "weights")
-    positions_at, other = _rows(positions, torch.int32, B, Hkv, top, "positions")
+    scores_at, stride = _rows(scores, _F32, B, Hkv, top, "scores")
+    weights_at, state_stride = _rows(weights, _F32, B, Hkv, top, "weights")
+    positions_at, other = _rows(positions, _I32, B, Hkv, top, "positions")
     if other != state_stride:
         raise ValueError("weights and positions: rows of one length are wanted")
-    rc = load().pillar_evict_kv(C.byref(s), scores_at, stride, decay, _tensor(old_lens, torch.int32, (B,), "old_lens"),
-                                _tensor(budgets, torch.int32, (B,), "budgets"), sink_tokens, recent_tokens, weights_at, positions_at,
-                                state_stride, _tensor(new_lens, torch.int32, (B,), "new_lens"), workspace.data_ptr(),
+    rc = load().pillar_evict_kv(C.byref(s), scores_at, stride, decay, _per_request(old_lens, B, "old_lens"),
+                                _per_request(budgets, B, "budgets"), sink_tokens, recent_tokens, weights_at, positions_at,
+                                state_stride, _per_request(new_lens, B, "new_lens"), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream(stream))
     _check(rc, "pillar_evict_kv")
 

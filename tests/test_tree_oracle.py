@@ -178,7 +178,7 @@ def test_the_binding_refuses_what_the_c_side_cannot_see():
             pb.pillar_tree_commit(kv, **{**commit, **bad})
     evict = dict(scores=rows, decay=0.5, old_lens=ints(B), budgets=ints(B), sink_tokens=1, recent_tokens=1, weights=rows.clone(), positions=ints(B, Hkv, 64),
                  new_lens=ints(B), workspace=ws)
-    for bad in (dict(positions=rows), dict(positions=ints(B, Hkv, 65)), dict(weights=rows[:, :, ::2]), dict(budgets=ints(B, 1)), dict(old_lens=None, weights=None)):
+    for bad in (dict(positions=rows), dict(positions=ints(B, Hkv, 65)), dict(weights=rows[:, :, ::2]), dict(budgets=ints(B + 1)), dict(new_lens=ints(B).long()), dict(old_lens=None, weights=None)):
         with pytest.raises((ValueError, pb.PillarError)):
             pb.pillar_evict_kv(kv, **{**evict, **bad})
 
