@@ -293,8 +293,8 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  *              nodes will do, and bits from tree_sizes[b] on are ignored).  Every
  *              node attends to all tokens before the tree.  A chain is
  *              visible[b][i] = 2^(i+1) - 1, plain decoding N = 1 and a word of 1.
- *   out, lse, scores, score_stride: as in pillar_verify_attn, the statistic being
- *              the mean over the tree_sizes[b]*G rows.  Slots from tree_sizes[b]
+ *   out, lse, scores, score_stride: as in pillar_verify_attn (no part of out may be
+ *              q), the statistic being the mean over the tree_sizes[b]*G rows.  Slots from tree_sizes[b]
  *              on and scores from seq_lens[b] on are not written, nor is anything
  *              of a request without nodes.  A node that sees no token gets out = 0
  *              and lse = -inf and adds nothing to the statistic.  What a node does
@@ -323,8 +323,8 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  * WRITES into the pools and, for fp8, into k_scale and v_scale: a page that
  * receives rows gets the largest scale that any of its rows up to the new length
  * had, and those rows are rounded anew to codes of that scale (at most half a
- * step of e4m3; where the scales are equal the bytes stay).  No page may belong to
- * two requests.  Pools and strides in multiples of 16 bytes, else
+ * step of e4m3; where the scales are equal the bytes stay).  No page that holds a
+ * node may belong to two requests.  Pools and strides in multiples of 16 bytes, else
  * PILLAR_EUNSUPPORTED. */
 size_t pillar_tree_workspace_bytes(const pillar_kv_t* kv, int32_t max_nodes);
 int pillar_verify_tree(const pillar_kv_t* kv, const void* q, int32_t max_nodes,

@@ -298,37 +298,52 @@ _Q_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 _F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
 
 
-def _refuse(t: torch.Tensor, what: str, wanted: str):
-    raise ValueError(f"{what}: a contiguous {wanted} is wanted, not {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ', strided'}")
+def _refuse(t: torch.Tensor, what: str, wanted: str, dev: int):
+    raise ValueError(f"{what}: a contiguous {wanted} on {'the CPU' if dev < 0 else f'cuda:{dev}'} is wanted, not {t.dtype} {tuple(t.shape)} on {t.device}"
+                     f"{'' if t.is_contiguous() else ', strided'}")
 
 
-# The address of a tensor whose type, shape and layout are what the C side takes for granted.  (A tenth of a microsecond per question asked: a
-# whole call takes eight.)
-def _tensor(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
+def _device(kv: KvCache) -> int:
+    """The GPU of the cache, which is the current one: work goes to its current stream."""
+    dev = kv.k_pool.get_device()
+    if dev >= 0 and dev != torch.cuda.current_device():
+        raise ValueError(f"the cache is on cuda:{dev}, which is not the current device")
+    return dev
+
+
+# The address of a tensor whose type, shape, layout and device are what the C side takes for granted.  (A tenth of a microsecond per question
+# asked: a whole call takes eight.)
+def _tensor(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, dev: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        _refuse(t, what, f"{dtype} tensor of shape {tuple(shape)}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, what, f"{dtype} tensor of shape {tuple(shape)}", dev)
     return t.data_ptr()
 
 
-def _per_request(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+def _per_request(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[int]:
     """int32, one entry per request."""
     if t is None:
         return None
-    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
-        _refuse(t, what, f"int32 tensor of {n}")
+    if t.dtype is not _I32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, what, f"int32 tensor of {n}", dev)
     return t.data_ptr()
 
 
-def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, B: int, Hkv: int, max_seq_len: int, what: str) -> tuple:
+def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, B: int, Hkv: int, max_seq_len: int, dev: int, what: str) -> tuple:
     """Address and stride of [B][Hkv][stride]: rows of at least max_seq_len entries, one behind the other."""
     if t is None:
         return None, 0
     shape = t.shape
-    if t.dtype is not dtype or len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < max_seq_len or not t.is_contiguous():
-        _refuse(t, what, f"{dtype} tensor [{B}, {Hkv}, >= {max_seq_len}]")
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < max_seq_len or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, what, f"{dtype} tensor [{B}, {Hkv}, >= {max_seq_len}]", dev)
     return t.data_ptr(), shape[2]
+
+
+def _scratch(t: torch.Tensor, dev: int) -> tuple:
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, "workspace", "tensor", dev)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def pillar_tree_workspace_bytes(kv: KvCache, max_nodes: int) -> int:
@@ -339,27 +354,24 @@ def pillar_tree_workspace_bytes(kv: KvCache, max_nodes: int) -> int:
 def pillar_verify_tree(kv: KvCache, q: torch.Tensor, tree_sizes: Optional[torch.Tensor], visible: torch.Tensor, out: torch.Tensor,
                        lse: Optional[torch.Tensor], scores: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     """visible: int64 [B, N], the bit patterns of the 64-bit words."""
-    s = kv.c_struct()
-    B, N = visible.shape
-    shape = (B, N, s.num_q_heads, s.head_dim)
-    if B != s.batch:
-        raise ValueError(f"visible: a row for each of {s.batch} requests is wanted, not {B}")
-    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, "scores")
-    rc = load().pillar_verify_tree(C.byref(s), _tensor(q, _Q_TORCH[kv.q_dtype], shape, "q"), N, _per_request(tree_sizes, B, "tree_sizes"),
-                                   _tensor(visible, _I64, (B, N), "visible"), _tensor(out, _Q_TORCH[kv.q_dtype], shape, "out"),
-                                   _tensor(lse, _F32, shape[:3], "lse"), scores_at, stride, workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _stream(stream))
+    s, dev = kv.c_struct(), _device(kv)
+    B, N = s.batch, visible.shape[-1]
+    shape, qt = (B, N, s.num_q_heads, s.head_dim), _Q_TORCH[kv.q_dtype]
+    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, dev, "scores")
+    rc = load().pillar_verify_tree(C.byref(s), _tensor(q, qt, shape, dev, "q"), N, _per_request(tree_sizes, B, dev, "tree_sizes"),
+                                   _tensor(visible, _I64, (B, N), dev, "visible"), _tensor(out, qt, shape, dev, "out"),
+                                   _tensor(lse, _F32, shape[:3], dev, "lse"), scores_at, stride, *_scratch(workspace, dev), _stream(stream))
     _check(rc, "pillar_verify_tree")
 
 
 def pillar_tree_commit(kv: KvCache, tree_sizes: Optional[torch.Tensor], max_nodes: int, path: torch.Tensor, path_lens: torch.Tensor,
                        new_lens: torch.Tensor, scores: Optional[torch.Tensor] = None, stream=None) -> None:
-    s = kv.c_struct()
+    s, dev = kv.c_struct(), _device(kv)
     B, M = s.batch, path.shape[-1]
-    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, "scores")
-    rc = load().pillar_tree_commit(C.byref(s), _per_request(tree_sizes, B, "tree_sizes"), max_nodes,
-                                   _tensor(path, _I32, (B, M), "path"), _per_request(path_lens, B, "path_lens"), M,
-                                   _per_request(new_lens, B, "new_lens"), scores_at, stride, _stream(stream))
+    scores_at, stride = _rows(scores, _F32, B, s.num_kv_heads, s.max_seq_len, dev, "scores")
+    rc = load().pillar_tree_commit(C.byref(s), _per_request(tree_sizes, B, dev, "tree_sizes"), max_nodes, _tensor(path, _I32, (B, M), dev, "path"),
+                                   _per_request(path_lens, B, dev, "path_lens"), M, _per_request(new_lens, B, dev, "new_lens"), scores_at, stride,
+                                   _stream(stream))
     _check(rc, "pillar_tree_commit")
 
 
@@ -371,17 +383,16 @@ def pillar_evict_workspace_bytes(kv: KvCache) -> int:
 def pillar_evict_kv(kv: KvCache, scores: Optional[torch.Tensor], decay: float, old_lens: torch.Tensor, budgets: torch.Tensor,
                     sink_tokens: int, recent_tokens: int, weights: torch.Tensor, positions: torch.Tensor, new_lens: torch.Tensor,
                     workspace: torch.Tensor, stream=None) -> None:
-    s = kv.c_struct()
+    s, dev = kv.c_struct(), _device(kv)
     B, Hkv, top = s.batch, s.num_kv_heads, s.max_seq_len
-    scores_at, stride = _rows(scores, _F32, B, Hkv, top, "scores")
-    weights_at, state_stride = _rows(weights, _F32, B, Hkv, top, "weights")
-    positions_at, other = _rows(positions, _I32, B, Hkv, top, "positions")
+    scores_at, stride = _rows(scores, _F32, B, Hkv, top, dev, "scores")
+    weights_at, state_stride = _rows(weights, _F32, B, Hkv, top, dev, "weights")
+    positions_at, other = _rows(positions, _I32, B, Hkv, top, dev, "positions")
     if other != state_stride:
         raise ValueError("weights and positions: rows of one length are wanted")
-    rc = load().pillar_evict_kv(C.byref(s), scores_at, stride, decay, _per_request(old_lens, B, "old_lens"),
-                                _per_request(budgets, B, "budgets"), sink_tokens, recent_tokens, weights_at, positions_at,
-                                state_stride, _per_request(new_lens, B, "new_lens"), workspace.data_ptr(),
-                                workspace.numel() * workspace.element_size(), _stream(stream))
+    rc = load().pillar_evict_kv(C.byref(s), scores_at, stride, decay, _per_request(old_lens, B, dev, "old_lens"),
+                                _per_request(budgets, B, dev, "budgets"), sink_tokens, recent_tokens, weights_at, positions_at, state_stride,
+                                _per_request(new_lens, B, dev, "new_lens"), *_scratch(workspace, dev), _stream(stream))
     _check(rc, "pillar_evict_kv")
 
 

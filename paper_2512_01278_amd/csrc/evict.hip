@@ -533,7 +533,8 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   ws.kept = reinterpret_cast<int32_t*>(p + w.kept);
   ws.edge = reinterpret_cast<float*>(p + w.edge);
   ws.list = reinterpret_cast<int32_t*>(p + w.list);
-  const int pairs = a.kv.batch * a.kv.num_kv_heads, esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
+  const int64_t pairs = static_cast<int64_t>(a.kv.batch) * a.kv.num_kv_heads;
+  const int esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
   const bool wide = a.state_stride % 4 == 0 && (!a.scores || a.score_stride % 4 == 0) &&
                     ((reinterpret_cast<uintptr_t>(a.weights) | reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.scores)) & 15u) == 0;
   // Where there is a workgroup for every compute unit it moves its rows too: a launch less.  (Not where the new lengths replace what the
@@ -561,7 +562,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     KernelTimer timer("evict_move", s);
     // at most half of the rows move; as many workgroups as that gives work, and no more than eight per compute unit
     const int most = (a.kv.max_seq_len / 2 + 15) / 16;
-    const int blocks = std::max(1, std::min(most, (8 * num_cus() + pairs - 1) / pairs));
+    const int blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, (8 * num_cus() + pairs - 1) / pairs)));
     const dim3 grid(blocks, a.kv.num_kv_heads, a.kv.batch);
     if (fp8) hipLaunchKernelGGL(evict_move<true>, grid, dim3(kMoveThreads), 0, s, a, ws, esz);
     else hipLaunchKernelGGL(evict_move<false>, grid, dim3(kMoveThreads), 0, s, a, ws, esz);

@@ -200,7 +200,7 @@ template <int D>
 __device__ __forceinline__ void see_nothing(const TreeParams& a, int b, int nodes) {
   const int64_t first = static_cast<int64_t>(b) * a.max_nodes * a.kv.num_q_heads;
   const int rows = nodes * a.kv.num_q_heads;
-  for (int e = threadIdx.x; e < rows * D; e += blockDim.x) {
+  for (int64_t e = threadIdx.x; e < static_cast<int64_t>(rows) * D; e += blockDim.x) {
     if (a.q_dtype == PILLAR_F32) Storage<PILLAR_F32>::store(a.out, first * D + e, 0.f);
     else Storage<PILLAR_BF16>::store(a.out, first * D + e, 0.f);
   }

@@ -227,6 +227,70 @@ def test_rows_past_32_bits():
     assert np.array_equal(k[-small:].view(torch.int16).cpu().numpy().view(np.uint16), want["k_pool"])
 
 
+@pytest.mark.parametrize("kv,D", [("bf16", 128), ("fp8_e4m3", 128), ("bf16", 64), ("fp8_e4m3", 64)])
+@pytest.mark.parametrize("N", [3, 12, 30, 50])
+def test_bounds_far_above_the_lengths(kv, D, N):
+    """Kernels are chosen by max_seq_len: with one that would mean gigabytes, rows bypass the cache and 50 nodes run on eight wavefronts."""
+    rng = np.random.default_rng(N)
+    w = make("bound", N, [N, 700, 64 + N, 1300], Hq=32, Hkv=8, D=D, P=64, kv=kv, extra_table_cols=400)
+    run = TreeRun(w, N, None, [ancestors(rng, N) for _ in range(4)], seed=N)
+    run.kv.max_seq_len = w.block_table.shape[1] * 64
+    run.scores = torch.full((4, 8, run.kv.max_seq_len), float("nan"), device=run.out.device)
+    run.workspace = torch.empty(pa.pillar_tree_workspace_bytes(run.kv, N), dtype=torch.uint8, device=run.out.device)
+    verified(run, f"bound {kv} {D} {N}")
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    runs = [tree_case("at once", [900, 300, 40], 9, seed=s) for s in (1, 2)]
+    for r in runs:
+        r.run()
+    torch.cuda.synchronize()
+    first = [(r.out.clone(), r.lse.clone()) for r in runs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for r, s in zip(runs, streams):
+            r.run(stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(r.out, f[0]) and torch.equal(r.lse, f[1]) for r, f in zip(runs, first))
+
+
+def test_one_workspace_for_two_graphs():
+    """Captured calls leave nothing behind that the other could trip over."""
+    runs = [tree_case("shared", [500, 80], 9, seed=1), tree_case("shared", [70, 900, 33], 17, seed=2, kv="fp8_e4m3")]
+    ws = max((r.workspace for r in runs), key=lambda t: t.numel())
+    graphs, first = [], []
+    for r in runs:
+        r.workspace = ws
+        r.run()
+        torch.cuda.synchronize()
+        first.append((r.out.clone(), r.lse.clone(), r.scores.clone()))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r.run()
+        graphs.append(g)
+    for turn in range(3):
+        for r, g, f in zip(runs, graphs, first):
+            for t in (r.out, r.lse, r.scores):
+                t.fill_(float("nan"))
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(r.out, f[0]) and torch.equal(r.lse, f[1]) and torch.equal(r.scores.nan_to_num(-1), f[2].nan_to_num(-1)), turn
+
+
+def test_tensors_of_another_device_are_refused():
+    run = tree_case("device", [40], 4)
+    for name in ("q", "out", "visible", "workspace"):
+        was = getattr(run, name)
+        setattr(run, name, was.cpu())
+        with pytest.raises(ValueError):
+            run.run()
+        setattr(run, name, was)
+    path, lens, now = torch.zeros(1, 2, dtype=torch.int32, device="cuda:0"), torch.zeros(1, dtype=torch.int32, device="cuda:0"), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        pa.pillar_tree_commit(run.kv, None, 4, path, lens, now)
+
+
 def test_streams_and_graphs():
     """Another stream than the current one; a captured call, replayed with eager work between, gives the bits of the eager call."""
     run = tree_case("graph", [800, 60, 9], 9, seed=12)
