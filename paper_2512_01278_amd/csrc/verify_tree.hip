@@ -221,7 +221,9 @@ struct Carrier {
   int pid[C::kLoads];
   u32x4 k[C::kLoads], v[V ? C::kLoads : 1];
   int scale_pid;
-  float ks, vs;
+  float ks, vs;                // page scales of a token: of the thread's own (bf16 engine) ...
+  static constexpr bool kRowScales = E::kF32 && C::KV == PILLAR_FP8_E4M3;
+  float row_ks[kRowScales ? C::kLoads : 1], row_vs[kRowScales ? C::kLoads : 1];                  // ... of each row that is carried (fp32)
 
   __device__ __forceinline__ Carrier(const KvView& kv, int b, int g, int len) {
     const int64_t head = static_cast<int64_t>(g) * kv.stride_head * kv_bytes<C::KV>();
@@ -240,12 +242,30 @@ struct Carrier {
     for (int u = 0; u < C::kLoads; ++u) pid[u] = carries() ? table[token(step, row(u)) >> kv.page_shift] : 0;
     if (C::kScales) scale_pid = table[token(step, min<int>(threadIdx.x, C::TS - 1)) >> kv.page_shift];
   }
+  __device__ __forceinline__ float k_scale(int u) const { return kRowScales ? row_ks[u] : 1.f; }
+  __device__ __forceinline__ float v_scale(int u) const { return kRowScales ? row_vs[u] : 1.f; }
   static __device__ __forceinline__ u32x4 load(const uint8_t* p) {
     if constexpr (C::kBypass) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
     else return *reinterpret_cast<const u32x4*>(p);
   }
-  // (strides below 2^32 bytes: a row's offset is two products of 32 bits)
-  __device__ __forceinline__ void fetch(const KvView& kv, int g, int step) {
+  __device__ __forceinline__ void fetch(const KvView& kv, int g, int step, bool aligned) {
+    if constexpr (E::kF32) {
+      if (!carries()) return;
+#pragma unroll
+      for (int u = 0; u < C::kLoads; ++u) {
+        const int64_t at = static_cast<int64_t>(g) * kv.stride_head + static_cast<int64_t>(pid[u]) * kv.stride_page +
+                           static_cast<int64_t>(token(step, row(u)) & (kv.page_size - 1)) * kv.stride_slot + piece * (16 / kv_bytes<C::KV>());
+        k[u] = load_piece<C::KV>(kv.k_pool, at, aligned);
+        if constexpr (V) v[u] = load_piece<C::KV>(kv.v_pool, at, aligned);
+        if constexpr (kRowScales) {
+          const int64_t s = static_cast<int64_t>(pid[u]) * kv.num_kv_heads + g;
+          row_ks[u] = kv.k_scale[s];
+          if constexpr (V) row_vs[u] = kv.v_scale[s];
+        }
+      }
+      return;
+    }
+    // (strides below 2^32 bytes: a row's offset is two products of 32 bits)
     const uint32_t page_bytes = static_cast<uint32_t>(kv.stride_page * kv_bytes<C::KV>()), slot_bytes = static_cast<uint32_t>(kv.stride_slot * kv_bytes<C::KV>());
     if (carries()) {
 #pragma unroll
@@ -325,11 +345,9 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
     float m_run = -INFINITY, l_run = 0.f;
 
     Carrier<C, true> c(kv, b, g, sh.len);
-    if constexpr (!E::kF32) {
-      c.pages(kv, s0);
-      c.fetch(kv, g, s0);
-      if (s0 + 1 < s1) c.pages(kv, s0 + 1);
-    }
+    c.pages(kv, s0);
+    c.fetch(kv, g, s0, a.aligned);
+    if (s0 + 1 < s1) c.pages(kv, s0 + 1);
 
     // What is not finite in a node's V counts for the rows that see the node only: it is left out of the tile, and added at the end.
     auto park_v = [&](const u32x4& x, float scale, int s, int r, int piece, bool tail) {
@@ -344,41 +362,19 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
 
     for (int s = s0; s < s1; ++s) {
       const bool tail = (s + 1) * TS > first_node;       // some token of the tile is a node, or past the end
-      // ---- the tile into LDS ----
-      if constexpr (!E::kF32) {
-        if (c.carries()) {
+      // ---- the tile into LDS, the next one on its way ----
+      if (c.carries()) {
 #pragma unroll
-          for (int i = 0; i < C::kLoads; ++i) {
-            const int r = c.row(i);
-            park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + r * E::kKPitch, c.piece);
-            park_v(c.v[i], 1.f, s, r, c.piece, tail);
-          }
-        }
-        if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
-      } else {
-#pragma unroll 4
         for (int i = 0; i < C::kLoads; ++i) {
-          const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
-          if (c.carries()) {
-            const int64_t at = static_cast<int64_t>(g) * kv.stride_head + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
-                               c.piece * (16 / kv_bytes<C::KV>());
-            const u32x4 kx = load_piece<C::KV>(kv.k_pool, at, a.aligned), vx = load_piece<C::KV>(kv.v_pool, at, a.aligned);
-            float ks = 1.f, vs = 1.f;
-            if constexpr (C::KV == PILLAR_FP8_E4M3) {
-              ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
-              vs = kv.v_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
-            }
-            park_piece<E, C::KV, false>(kx, ks, ktile + r * E::kKPitch, c.piece);
-            park_v(vx, vs, s, r, c.piece, tail);
-          }
+          park_piece<E, C::KV, false>(c.k[i], c.k_scale(i), ktile + c.row(i) * E::kKPitch, c.piece);
+          park_v(c.v[i], c.v_scale(i), s, c.row(i), c.piece, tail);
         }
       }
+      if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
       __syncthreads();
-      if constexpr (!E::kF32) {
-        if (s + 1 < s1) {
-          c.fetch(kv, g, s + 1);
-          if (s + 2 < s1) c.pages(kv, s + 2);
-        }
+      if (s + 1 < s1) {
+        c.fetch(kv, g, s + 1, a.aligned);
+        if (s + 2 < s1) c.pages(kv, s + 2);
       }
       if (s == s0 && tid < 2) s_bad[parity ^ 1][tid] = 0;
 
@@ -635,7 +631,7 @@ __global__ __launch_bounds__(128) void tree_merge(TreeParams a) {
 // the same threads wrote before. ----
 // wavefronts per SIMD that the statistic's kernel is compiled for: what the registers allow without spilling
 template <typename C>
-constexpr int score_waves() { return C::E::kF32 || C::WR == 1 ? 2 : C::WR == 8 ? 4 : 3; }
+constexpr int score_waves() { return C::E::kF32 && C::WR == 1 && C::D == 128 ? 1 : C::E::kF32 || C::WR == 1 ? 2 : C::WR == 8 ? 4 : 3; }
 
 template <typename C>
 __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(TreeParams a, float* scores, int64_t score_stride) {
@@ -684,42 +680,24 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
         s_y[wr * 32 + n] = mine;
         s_word[wr * 32 + n] = there ? a.visible[static_cast<int64_t>(b) * a.max_nodes + node] : 0;
       }
-      if constexpr (!E::kF32) {
-        c.pages(kv, s0);
-        c.fetch(kv, g, s0);
-        if (s0 + 1 < s1) c.pages(kv, s0 + 1);
-      }
+      c.pages(kv, s0);
+      c.fetch(kv, g, s0, a.aligned);
+      if (s0 + 1 < s1) c.pages(kv, s0 + 1);
       __syncthreads();
       float y[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = s_y[wr * 32 + elem_of(i, g2)];
 
       for (int s = s0; s < s1; ++s) {
-        if constexpr (!E::kF32) {
-          if (c.carries()) {
+        if (c.carries()) {
 #pragma unroll
-            for (int i = 0; i < C::kLoads; ++i) park_piece<E, C::KV, false>(c.k[i], 1.f, ktile + c.row(i) * E::kKPitch, c.piece);
-          }
-          if (C::kScales && tid < TS) s_ks[tid] = c.ks;
-        } else {
-#pragma unroll 4
-          for (int i = 0; i < C::kLoads; ++i) {
-            const int r = c.row(i), t = c.token(s, r), p = c.table[t >> kv.page_shift];
-            if (c.carries()) {
-              const int64_t at = static_cast<int64_t>(g) * kv.stride_head + static_cast<int64_t>(p) * kv.stride_page + static_cast<int64_t>(t & (kv.page_size - 1)) * kv.stride_slot +
-                                 c.piece * (16 / kv_bytes<C::KV>());
-              float ks = 1.f;
-              if constexpr (C::KV == PILLAR_FP8_E4M3) ks = kv.k_scale[static_cast<int64_t>(p) * kv.num_kv_heads + g];
-              park_piece<E, C::KV, false>(load_piece<C::KV>(kv.k_pool, at, a.aligned), ks, ktile + r * E::kKPitch, c.piece);
-            }
-          }
+          for (int i = 0; i < C::kLoads; ++i) park_piece<E, C::KV, false>(c.k[i], c.k_scale(i), ktile + c.row(i) * E::kKPitch, c.piece);
         }
+        if (C::kScales && tid < TS) s_ks[tid] = c.ks;
         __syncthreads();
-        if constexpr (!E::kF32) {
-          if (s + 1 < s1) {
-            c.fetch(kv, g, s + 1);
-            if (s + 2 < s1) c.pages(kv, s + 2);
-          }
+        if (s + 1 < s1) {
+          c.fetch(kv, g, s + 1, a.aligned);
+          if (s + 2 < s1) c.pages(kv, s + 2);
         }
 #pragma unroll
         for (int sub = 0; sub < C::NS; ++sub) {
@@ -772,9 +750,9 @@ TreePlan plan_of(const KvView& kv, int max_nodes, bool f32) {
   const int groups = (rows + 31) / 32;
   int per_cu;
   if (f32) {
-    p.rt = groups <= 1 ? 32 : 128;
+    p.rt = groups <= 1 ? 32 : groups <= 2 ? 64 : 128;
     p.ts = groups <= 1 ? 128 : 64;
-    per_cu = 1;
+    per_cu = kv.head_dim == 64 ? 2 : 1;
   } else {
     // 256 rows to a workgroup read K and V once for them, 128 make twice as many units: one request of 2100 tokens with 60 nodes 36 / 30 us, 4 49 / 40,
     // 128 of 1-8 K tokens 788 / 992
@@ -865,6 +843,7 @@ hipError_t launch_bf16(const TreeParams& p, const TreePlan& plan, const TreeArgs
 template <int D, int KV>
 hipError_t launch_f32(const TreeParams& p, const TreePlan& plan, const TreeArgs& t, hipStream_t s) {
   if (plan.rt == 32) return launch_tree<Cfg<D, KV, true, 1, 4, 1, false>>(p, plan, t, s);
+  if (plan.rt == 64) return launch_tree<Cfg<D, KV, true, 2, 2, 1, false>>(p, plan, t, s);
   return launch_tree<Cfg<D, KV, true, 4, 1, 2, false>>(p, plan, t, s);
 }
 
