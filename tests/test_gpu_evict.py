@@ -90,11 +90,21 @@ def test_lengths(n, keep):
     State(w, n, few=True).check([n // 2], [keep], 4, 64, what=f"{n} ties")
 
 
-def test_many_requests():
+@pytest.mark.parametrize("alias", [None, "old", "budgets", "lens"])
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+def test_many_requests(kv, alias):
+    """More (request, KV head) pairs than compute units: rows move in the launch that selects, unless the new lengths replace what it reads."""
     rng = np.random.default_rng(2)
     lens = rng.integers(1, 200, size=90)
-    w = make("many", 3, lens, Hq=4, Hkv=4, D=64, kv="fp8_e4m3")
-    State(w, 13).check(rng.integers(0, 200, size=90), rng.integers(0, 150, size=90), 2, 5, what="many")
+    w = make("many", 3, lens, Hq=4, Hkv=4, D=64, kv=kv)
+    State(w, 13).check(rng.integers(0, 200, size=90), rng.integers(0, 150, size=90), 2, 5, alias=alias, what="many")
+
+
+@pytest.mark.parametrize("n,keep", [(3000, 2990), (9000, 5000), (33000, 32000)])
+@pytest.mark.parametrize("P", [1, 32, 256])
+def test_long_rows_of_fp8(n, keep, P):
+    w = make("long8", 3, [n, n // 3], Hq=1, Hkv=1, D=64, kv="fp8_e4m3", P=P)
+    State(w, n).check([n // 2, 0], [keep, n // 7], 4, 64, what=f"{n} P={P}")
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
