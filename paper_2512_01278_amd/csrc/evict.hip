@@ -11,8 +11,8 @@
 //
 // One or two launches:
 //   evict_select  one workgroup per (request, KV head): the weights, a radix select of the K'-th key, the list of holes and sources in
-//                 order, the moves within weights and positions, and, where the launch fills the chip, the rows of K and V;
-//   evict_move    else, the rows of K and V by workgroups of their own.
+//                 order, the moves within weights and positions, and the rows of K and V, unless few workgroups would have many to move:
+//   evict_move    then, workgroups of their own.
 //
 // A step at the budget moves a few rows: it is as long as a chain of loads (lengths, state, page ids, rows), two histograms and their
 // barriers.  So the keys stay in registers from one load on, and a digit of the K'-th key that all its keys survive ends the search (the
@@ -537,10 +537,12 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   const int esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
   const bool wide = a.state_stride % 4 == 0 && (!a.scores || a.score_stride % 4 == 0) &&
                     ((reinterpret_cast<uintptr_t>(a.weights) | reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.scores)) & 15u) == 0;
-  // Where there is a workgroup for every compute unit it moves its rows too: a launch less.  (Not where the new lengths replace what the
+  // One launch, in which the workgroup that selects moves its rows too, where that fills the chip or the rows are short; else few workgroups would
+  // move many rows.  Two / one: 64 requests, 5 of 4101 tokens, 22 / 18 us, one, 2 of 2050 15 / 13, 2048 of 4096 16 / 13, 31, 16 of 8016 20 / 17;
+  // fp8: 8, 4 of 4004 25 / 16, one, 2048 of 4096 37 / 44; one, 20000 of 21000 30 / 37.  (Not where the new lengths replace what the
   // workgroups of other heads read.)
   auto apart = [&](const int32_t* p) { return a.new_lens + a.kv.batch <= p || p + a.kv.batch <= a.new_lens; };
-  const bool moves_rows = pairs >= num_cus() && apart(a.kv.seq_lens) && apart(a.old_lens) && apart(a.budgets);
+  const bool moves_rows = (pairs >= num_cus() || a.kv.max_seq_len <= 8192) && apart(a.kv.seq_lens) && apart(a.old_lens) && apart(a.budgets);
   const bool fp8 = a.kv_dtype == PILLAR_FP8_E4M3;
   {
     KernelTimer timer("evict_select", s);
