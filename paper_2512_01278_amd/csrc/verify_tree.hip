@@ -41,6 +41,7 @@ struct TreeParams {
   float* part_o;               // [slots][RT][D]
   float* lse2;                 // [B][max_nodes][Hq], in log2 units; only with scores
   int32_t ranges, few;         // workgroups of the pass; of those, with little to do
+  int32_t tiles8;              // eight times the tiles there may be, or the largest number where a tile may go into ranges of one unit
 };
 
 // Units are counted the same way by the pass and the merge.
@@ -68,12 +69,20 @@ __device__ __forceinline__ int units_of(const TreeParams& a, int b) {
 // compute unit: one request of 8000 tokens with 26 nodes 42 / 33 us, 4 of 2100 38 / 32, with 60 nodes 48 / 40, 8 of 2100 46 / 39; 16 of 4000
 // (16 units each) 78 / 79, 32 of 4096 with 32 nodes 118 / 130.
 constexpr int kFewUnits = 8;
+// And never so many that a tile's partials take longer to join than its units: with U units to a tile, a range has sqrt(U / 8) of them at the least.  One
+// unit / the rule: one request of 2100 tokens (33 units) with 26 nodes 25.7 / 22.2 us, with 60 34.0 / 28.5, of 20000 with one kv head 48 / 29.5;
+// of 8000 with 8 kv heads and 500 the same; with one node 15.2 / 17.  sqrt(U / 4) and sqrt(U / 16) are slower by up to 3.  An fp32 unit takes
+// far longer than the joining of a partial: 2 of 2100 tokens with 26 nodes 35 / 48, so there the rule is off.
+constexpr int kMostUnits = 16;                           // (where the root is more, the number of workgroups decides)
 
 // Range w of n has units range_begin(w) .. range_begin(w + 1) - 1.
 struct Ranges {
   int n, each, longer;         // the first `longer` ranges have each + 1 units, the others `each`
-  __device__ __forceinline__ Ranges(int total, int workgroups, int few) {
-    n = max(1, min(total, total < kFewUnits * workgroups ? few : workgroups));
+  __device__ __forceinline__ Ranges(int total, int workgroups, int few, int tiles8) {
+    const int eighth = (total - 1) / tiles8;
+    int least = 1;                                       // sqrt(total / tiles8), rounded up; in integers, so that all kernels agree
+    while (least < kMostUnits && least * least <= eighth) ++least;
+    n = max(1, min(total / least, total < kFewUnits * workgroups ? few : workgroups));
     each = total / n;
     longer = total - each * n;
   }
@@ -101,7 +110,7 @@ struct Share {
   int b, ub;                   // the request that has unit u0, and that request's first unit
   // units: of a request; each(c): called for every 64 requests; prefix: the first workgroup leaves the units before every request, and all of them, there
   template <typename F, typename Each>
-  __device__ __forceinline__ Share(int batch, int workgroups, int few, int32_t* prefix, F units, Each each) {
+  __device__ __forceinline__ Share(int batch, int workgroups, int few, int tiles8, int32_t* prefix, F units, Each each) {
     const int lane = threadIdx.x & 63;
     int total = 0, mine = 0, upto = 0;
     for (int c = 0; c < batch; c += 64) {
@@ -110,7 +119,7 @@ struct Share {
       total = __builtin_amdgcn_readlane(upto, 63);
       each(c);
     }
-    const Ranges ranges(total, workgroups, few);
+    const Ranges ranges(total, workgroups, few, tiles8);
     // neighbouring ranges, whose row tiles may share K and V, on one XCD (workgroups go round the XCDs in turn)
     w = blockIdx.x;
     u0 = u1 = b = ub = 0;
@@ -300,7 +309,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   uint8_t* const vtile = smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
 
-  const Share share(kv.batch, a.ranges, a.few, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
+  const Share share(kv.batch, a.ranges, a.few, a.tiles8, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
     // contexts without a token have no unit: their rows are shared out among the workgroups
     for (uint64_t none = __ballot(c + lane < kv.batch && kv.seq_lens[min(c + lane, kv.batch - 1)] <= 0); none; none &= none - 1) {
       const int r = c + __builtin_ctzll(none);
@@ -561,7 +570,7 @@ __global__ __launch_bounds__(128) void tree_merge(TreeParams a) {
   constexpr int kLanes = D / 4, kRows = 128 / kLanes;
   const KvView& kv = a.kv;
   const int lane = threadIdx.x & 63, part = threadIdx.x % kLanes;
-  const Ranges ranges(a.prefix[kv.batch], a.ranges, a.few);
+  const Ranges ranges(a.prefix[kv.batch], a.ranges, a.few, a.tiles8);
   const int w = blockIdx.x + 1;
   if (w >= ranges.n) return;
   const int u = ranges.begin(w);
@@ -646,7 +655,7 @@ __global__ __launch_bounds__(C::kThreads, score_waves<C>()) void tree_scores(Tre
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % C::WR, wt = wave / C::WR, n = lane & 31, g2 = lane >> 5;
   const float scale2 = kv.sm_scale * kLog2e;
-  const Share share(kv.batch, gridDim.x, gridDim.x, nullptr, [&](int r) {
+  const Share share(kv.batch, gridDim.x, gridDim.x, INT32_MAX, nullptr, [&](int r) {
     const Shape sh = shape_of<TS, RT>(a, r);
     return sh.rows > 0 ? sh.steps * kv.num_kv_heads : 0;
   }, [](int) {});
@@ -887,6 +896,7 @@ hipError_t launch_verify_tree(const TreeArgs& t, hipStream_t s) {
   p.lse2 = t.scores ? reinterpret_cast<float*>(ws + w.lse2) : nullptr;
   p.ranges = plan.ranges;
   p.few = std::min(plan.ranges, num_cus());
+  p.tiles8 = f32 ? INT32_MAX : static_cast<int32_t>(std::min<int64_t>(8 * plan.tiles, INT32_MAX));
   const bool wide = kv.head_dim == 128;
   if (!f32) {
     if (t.kv_dtype == PILLAR_BF16) return wide ? launch_bf16<128, PILLAR_BF16>(p, plan, t, s) : launch_bf16<64, PILLAR_BF16>(p, plan, t, s);
