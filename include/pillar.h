@@ -293,13 +293,13 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  *              nodes will do, and bits from tree_sizes[b] on are ignored).  Every
  *              node attends to all tokens before the tree.  A chain is
  *              visible[b][i] = 2^(i+1) - 1, plain decoding N = 1 and a word of 1.
- *   out, lse, scores, score_stride: as in pillar_verify_attn (no part of out may be
- *              q), the statistic being the mean over the tree_sizes[b]*G rows.  Slots from tree_sizes[b]
- *              on and scores from seq_lens[b] on are not written, nor is anything
- *              of a request without nodes.  A node that sees no token gets out = 0
- *              and lse = -inf and adds nothing to the statistic.  What a node does
- *              not see has no influence on it, whatever the cache holds there
- *              (infinities and NaN included).
+ *   out, lse, scores, score_stride: as in pillar_verify_attn, the statistic being
+ *              the mean over the tree_sizes[b]*G rows; no part of out may be q
+ *              (PILLAR_EINVAL).  Slots from tree_sizes[b] on and scores from
+ *              seq_lens[b] on are not written, nor is anything of a request without
+ *              nodes.  A node that sees no token gets out = 0 and lse = -inf and adds
+ *              nothing to the statistic.  What a node does not see has no influence
+ *              on it, whatever the cache holds there (infinities and NaN included).
  * Every shape that pillar_kv_t can describe, page sizes of 1 on, group sizes up
  * to 16, with up to 1024 rows per KV head.  bf16 queries with a bf16 or fp8 cache
  * run on bf16 matrix instructions (P is rounded to bf16), if q, out, the pools and
@@ -345,6 +345,8 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
  *   weights    device [B][Hkv][state_stride] fp32, in and out:
  *              w[t] <- decay * w[t] + scores[t] for t < o, scores[t] for o <= t < L.
  *              scores NULL: the weights of old tokens stay, new ones get 0.
+ *              (A verification leaves the scores of a request without nodes as
+ *              they were: clear them where there may be one.)
  *   positions  device [B][Hkv][state_stride] int32, in and out: the place of each
  *              cached token in the text.  New tokens are numbered on from the
  *              largest of the old ones (from 0 where there is none).

@@ -308,6 +308,8 @@ def _device(kv: KvCache) -> int:
     dev = kv.k_pool.get_device()
     if dev >= 0 and dev != torch.cuda.current_device():
         raise ValueError(f"the cache is on cuda:{dev}, which is not the current device")
+    if dev < 0 and torch.cuda.is_available():
+        raise ValueError("the cache is in host memory")
     return dev
 
 

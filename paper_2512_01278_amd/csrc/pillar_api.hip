@@ -132,6 +132,11 @@ bool rows_in_pieces(const pillar_kv_t* kv) {
          ((reinterpret_cast<uintptr_t>(kv->k_pool) | reinterpret_cast<uintptr_t>(kv->v_pool)) & 15u) == 0;
 }
 
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
+
 // requests and heads are the second and third dimension of a grid
 bool fits_a_grid(const pillar_kv_t* kv) { return kv->batch <= 65535 && kv->num_kv_heads <= 65535; }
 
@@ -512,6 +517,9 @@ int pillar_verify_tree(const pillar_kv_t* kv, const void* q, int32_t max_nodes, 
   if (!verify_tree_counts(a.kv, max_nodes)) return PILLAR_EUNSUPPORTED;
   rc = check_workspace(workspace, workspace_bytes, verify_tree_workspace(a.kv, max_nodes));
   if (rc != PILLAR_OK) return rc;
+  // several workgroups read a row of q, and one of them writes its result
+  const uint64_t bytes = static_cast<uint64_t>(kv->batch) * max_nodes * kv->num_q_heads * kv->head_dim * (kv->q_dtype == PILLAR_F32 ? 4 : 2);
+  if (overlap(q, bytes, out, bytes)) return PILLAR_EINVAL;
   a.q = q;
   a.tree_sizes = tree_sizes;
   a.visible = visible;
@@ -537,8 +545,8 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
   if (max_path > tree_nodes_max()) return PILLAR_EUNSUPPORTED;
   if (scores && score_stride < kv->max_seq_len) return PILLAR_EINVAL;
   // the heads of a request read its length while one of them writes the new one
-  const uintptr_t lens = reinterpret_cast<uintptr_t>(kv->seq_lens), now = reinterpret_cast<uintptr_t>(new_lens), span = static_cast<uintptr_t>(kv->batch) * 4;
-  if (now < lens + span && lens < now + span) return PILLAR_EINVAL;
+  const uint64_t span = static_cast<uint64_t>(kv->batch) * 4;
+  if (overlap(kv->seq_lens, span, new_lens, span)) return PILLAR_EINVAL;
   if (!rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
   CommitArgs a;
   a.kv = make_view(kv);

@@ -1,4 +1,6 @@
 """Trees of drafted tokens on the GPU against the oracle: every kernel, head layout, page size and mask where they can go wrong."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -286,6 +288,10 @@ def test_tensors_of_another_device_are_refused():
         with pytest.raises(ValueError):
             run.run()
         setattr(run, name, was)
+    kv, run.kv = run.kv, dataclasses.replace(run.kv, k_pool=run.kv.k_pool.cpu())
+    with pytest.raises(ValueError):
+        run.run()
+    run.kv = kv
     path, lens, now = torch.zeros(1, 2, dtype=torch.int32, device="cuda:0"), torch.zeros(1, dtype=torch.int32, device="cuda:0"), torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError):
         pa.pillar_tree_commit(run.kv, None, 4, path, lens, now)

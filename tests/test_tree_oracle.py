@@ -118,6 +118,7 @@ def test_tree_arguments(lib):  # noqa: F811
     need = lambda kv, n: lib.pillar_tree_workspace_bytes(C.byref(kv), n)
     assert need(s, 8) > 0 and need(s, 8) % 256 == 0 and need(s, 0) == need(s, 65) == need(good_kv(batch=0), 8) == 0
     assert vt(wsz=need(s, 8) - 1) == pb.PILLAR_EWORKSPACE
+    assert vt() == vt(out=FAKE + 16) == vt(q=FAKE + 16) == pb.PILLAR_EINVAL                    # queries that would be written over
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(num_q_heads=128), dict(num_q_heads=8, head_dim=64), dict(q_dtype=pb.PILLAR_F32, kv_dtype=pb.PILLAR_F32)])
