@@ -148,6 +148,13 @@ def test_contexts_cut_into_many_ranges(N, kv):
     verified(tree_case("long", [5000 + N, N, 700, 64 + N], N, kv=kv, Hq=4, Hkv=1, seed=N), f"long {N} {kv}")
 
 
+@pytest.mark.parametrize("lens,sizes", [([20001], None), ([12345, 3, 0, 6400], None), ([9000, 8999, 64], [0, 5, 1])])
+@pytest.mark.parametrize("N,kv", [(5, "bf16"), (40, "bf16"), (13, "fp8_e4m3")])
+def test_ranges_of_several_units(lens, sizes, N, kv):
+    """One KV head and few requests: a range is several units long, and a tile has partials of a dozen or more."""
+    verified(tree_case("several", lens, N, kv=kv, Hq=4, Hkv=1, sizes=sizes, seed=N), f"several {lens} {N} {kv}")
+
+
 @pytest.mark.parametrize("N", [1, 10, 40])
 def test_more_requests_than_a_wavefront_has_lanes(N):
     rng = np.random.default_rng(N)
