@@ -11,8 +11,8 @@
 //
 // Two engines share the code around them:
 //   EngineBf16   bf16 queries, bf16 or fp8 cache: v_mfma_f32_32x32x16_bf16; fp8 rows are widened (exactly) on the way into LDS, their page
-//                scales are applied to the logits and to P in fp32.  P is rounded to bf16 (at most 2^-9 of each probability), as the matrix
-//                cores take it; sums of P are those of the unrounded values.
+//                scales are applied in fp32, v_scale as a summand of the logits in log2.  P is rounded to bf16 (at most 2^-8 of each
+//                probability), as the matrix cores take it; sums of P are those of the unrounded values.
 //   EngineF32    anything: rows become fp32 in LDS (fp8 times its scale), v_mfma_f32_32x32x2_f32.
 //
 // LDS rows are padded: K by 16 bytes, so that the 16-byte pieces that 16 rows hold at one place cover all banks; V so that the four rows of a

@@ -298,7 +298,8 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   using E = typename C::E;
   constexpr int D = C::D, TS = C::TS, RT = C::RT;
   __shared__ __attribute__((aligned(16))) uint8_t smem[C::kLds];
-  __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? TS : 4], s_vs[C::kScales ? TS : 4];
+  // page scales of the tile's tokens: k_scale in the logits' unit, log2 of v_scale, and one over it
+  __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? TS : 4], s_log_vs[C::kScales ? TS : 4], s_inv_vs[C::kScales ? TS : 4];
   __shared__ float s_m[C::kWaves][32], s_l[C::kWaves][32];
   __shared__ uint32_t s_bad[2][2];                       // nodes whose V row is not finite throughout
   const KvView& kv = a.kv;
@@ -308,6 +309,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
   uint8_t* const ktile = smem;
   uint8_t* const vtile = smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
+  const float unit = C::kScales ? 1.f : scale2;          // of the logits, in log2: page scales come with it
 
   const Share share(kv.batch, a.ranges, a.few, a.tiles8, a.prefix, [&](int r) { return units_of<TS, RT>(a, r); }, [&](int c) {
     // contexts without a token have no unit: their rows are shared out among the workgroups
@@ -379,7 +381,15 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
           park_v(c.v[i], c.v_scale(i), s, c.row(i), c.piece, tail);
         }
       }
-      if (C::kScales && tid < TS) { s_ks[tid] = c.ks; s_vs[tid] = c.vs; }
+      // With v_scale in the exponent the weightiest p v_scale of a tile is 1, which bf16 has exactly; as a factor on P it left the weight of a row that
+      // one token dominates off by 2^-8 (64 fp8 requests, out against 64 bits: 0.0024 of its norm, now 0.0018 of which 0.0017 is out's own
+      // rounding; 611 / 637 us).
+      if (C::kScales && tid < TS) {
+        const float log_vs = __builtin_amdgcn_logf(c.vs < 0x1p-100f ? 0x1p-100f : c.vs);      // (zero: as small as l can carry)
+        s_ks[tid] = c.ks * scale2;
+        s_log_vs[tid] = log_vs;
+        s_inv_vs[tid] = fast_exp2(-log_vs);              // (of the rounded logarithm: l is exact to fp32)
+      }
       __syncthreads();
       if (s + 1 < s1) {
         c.fetch(kv, g, s + 1, a.aligned);
@@ -402,8 +412,9 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
               const f32x4 f = *reinterpret_cast<const f32x4*>(s_ks + at + 32 * sub + elem_of(i, g2));
+              const f32x4 d = *reinterpret_cast<const f32x4*>(s_log_vs + at + 32 * sub + elem_of(i, g2));
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[sub][i + j] *= f[j];
+              for (int j = 0; j < 4; ++j) x[sub][i + j] = __builtin_fmaf(x[sub][i + j], f[j], d[j]);
             }
           }
         }
@@ -432,7 +443,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
         for (int sub = 0; sub < C::NS; ++sub)
 #pragma unroll
           for (int i = 0; i < 16; ++i) top = fmaxf(top, x[sub][i]);
-        top = other_half_max(top) * scale2;
+        top = other_half_max(top) * unit;
         // The maximum that exponentials are relative to moves only when a logit exceeds it by more than 8 (in log2 units): P stays below
         // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.
         if (__any(top > m_run + 8.f)) {
@@ -451,19 +462,20 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
         for (int sub = 0; sub < C::NS; ++sub) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            x[sub][i] = fast_exp2(__builtin_fmaf(x[sub][i], scale2, -m_use));
-            sum[i & 1] += x[sub][i];
+            x[sub][i] = fast_exp2(C::kScales ? x[sub][i] - m_use : __builtin_fmaf(x[sub][i], scale2, -m_use));
+            if (!C::kScales) sum[i & 1] += x[sub][i];
           }
           if constexpr (C::kScales) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(s_vs + at + 32 * sub + elem_of(i, g2));
+              const f32x4 f = *reinterpret_cast<const f32x4*>(s_inv_vs + at + 32 * sub + elem_of(i, g2));
+              if (masked) {                              // (the scale of a page that no row sees may be anything)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[sub][i + j] *= f[j];
-            }
-            if (masked) {                                // (the scale of a page that no row sees may be anything)
+                for (int j = 0; j < 4; ++j) sum[j & 1] += (sees[sub] >> elem_of(i + j, 0) & 1u) ? x[sub][i + j] * f[j] : 0.f;
+              } else {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) x[sub][i] = (sees[sub] >> elem_of(i, 0) & 1u) ? x[sub][i] : 0.f;
+                for (int j = 0; j < 4; ++j) sum[j & 1] = __builtin_fmaf(x[sub][i + j], f[j], sum[j & 1]);
+              }
             }
           }
           E::pv(vtile + (at + 32 * sub) * E::kVPitch, x[sub], o, lane);
@@ -807,7 +819,7 @@ bool rows_aligned(const KvView& kv, int kv_dtype) {
 
 template <typename C>
 hipError_t launch_tree(const TreeParams& p, const TreePlan& plan, const TreeArgs& t, hipStream_t s) {
-  static_assert(C::kLds + 2 * C::TS * 4 + 64 * C::kWaves * 4 + 64 <= 160 * 1024, "");
+  static_assert(C::kLds + 12 * C::TS + 64 * C::kWaves * 4 + 64 <= 160 * 1024, "");
   {
     KernelTimer timer("tree_pass", s);
     hipLaunchKernelGGL((tree_pass<C>), dim3(p.ranges), dim3(C::kThreads), 0, s, p);
