@@ -57,4 +57,10 @@ __host__ __device__ inline bool draft_bypasses(int64_t list_rows, bool fp8) { re
 // 339, 32 426 / 417; fp8 202 / 191, 209 / 201, 380 / 375; 8 nodes with the statistic, which reads K again, 590 / 540.
 inline bool tree_bypasses(int64_t bytes) { return bytes > (int64_t{128} << 20); }
 
+// The nodes of a tree that two words of 32 bits name, nodes 0 to 31 and 32 to 63.  (The words come out of scalar registers as signed numbers: widened as
+// such, node 31 would name nodes 32 to 63 too.)
+__host__ __device__ inline uint64_t nodes_of(int32_t low, int32_t high) {
+  return static_cast<uint32_t>(low) | static_cast<uint64_t>(static_cast<uint32_t>(high)) << 32;
+}
+
 }  // namespace pillar

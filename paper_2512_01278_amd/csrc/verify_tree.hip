@@ -486,9 +486,10 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
       __syncthreads();
     }
 
-    const uint64_t bad = __builtin_amdgcn_readfirstlane(s_bad[parity][0]) | static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(s_bad[parity][1])) << 32;
+    const uint64_t bad = nodes_of(__builtin_amdgcn_readfirstlane(s_bad[parity][0]), __builtin_amdgcn_readfirstlane(s_bad[parity][1]));
     for (uint64_t left = bad; left; left &= left - 1) {
       const int j = __builtin_ctzll(left), t = first_node + j;
+      if (t >= sh.len) break;                            // (there is no such row)
       if ((t % TS) / C::kGroupTokens != wt) continue;    // (the wavefronts whose maximum has seen the token)
       int page;
       const int64_t at = row_offset(kv, b, g, t, &page);
