@@ -445,11 +445,12 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
           for (int i = 0; i < 16; ++i) top = fmaxf(top, x[sub][i]);
         top = other_half_max(top) * unit;
         // The maximum that exponentials are relative to moves only when a logit exceeds it by more than 8 (in log2 units): P stays below
-        // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.
-        if (__any(top > m_run + 8.f)) {
-          const float m_new = fmaxf(m_run, top);
-          const float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
-          m_run = m_new;
+        // 2^8, which costs no precision in floating point, and the accumulators are rescaled a few times per stretch.  Each row goes by its own
+        // logits: what other rows see moves no bit of it.
+        const bool moves = top > m_run + 8.f;
+        if (__any(moves)) {
+          const float f = !moves ? 1.f : m_run == -INFINITY ? 0.f : fast_exp2(m_run - top);
+          m_run = moves ? top : m_run;
           l_run *= f;
 #pragma unroll
           for (int db = 0; db < D / 32; ++db)

@@ -50,3 +50,37 @@ def test_nodes_at_the_ends_of_the_words(kv, flags, N, hit):
         assert not torch.isfinite(seen[..., ::3]).any()
         for dim in (1, 2):
             assert torch.equal(seen[..., dim::3], clean.out[:, j].float()[..., dim::3])
+
+
+@pytest.mark.parametrize("kv,flags", TYPES)
+@pytest.mark.parametrize("Hq,N", [(4, 8), (4, 12), (4, 30), (8, 40)])
+def test_keys_that_one_node_sees(kv, flags, Hq, N):
+    """K of the last two nodes, each seen by itself only, infinite in one dimension, then finite and large: nobody else's logits have them, so nobody
+    else's running maximum moves.  (A page of one token each: an fp8 row is made large by its scale.)"""
+    lens, q = [N + 3, 300, 1500], "f32" if kv == "f32" else "bf16"
+    rng = np.random.default_rng(N)
+    w = make("keys", 32, lens, Hq=Hq, Hkv=1, D=64, P=1, kv=kv, q=q)
+    words = alone([ancestors(rng, N) for _ in lens], [N - 2, N - 1])
+    clean = TreeRun(w, N, None, words, seed=N, flags=flags)
+    clean.run()
+    torch.cuda.synchronize()
+    for what in ("large",) if kv == "fp8_e4m3" else ("inf", "large"):
+        print(f"[case] {what} Hq={Hq} N={N} {kv} flags={flags}", flush=True)
+        k, scale = w.k_pool.copy(), None if w.k_scale is None else w.k_scale.copy()
+        for b, n in enumerate(lens):
+            for t in (n - 2, n - 1):
+                if what == "inf":
+                    set_row(w, w.k_pool, b, t, STORED[kv]["inf"], 5)
+                elif kv == "fp8_e4m3":
+                    w.k_scale[w.block_table[b, t]] *= 1024
+                elif kv == "bf16":
+                    w.k_pool[w.block_table[b, t]] += np.uint16(10 << 7)            # the exponent
+                else:
+                    w.k_pool[w.block_table[b, t]] *= 1024
+        dirty = TreeRun(w, N, None, words, seed=N, flags=flags)
+        dirty.run()
+        torch.cuda.synchronize()
+        w.k_pool, w.k_scale = k, scale
+        assert torch.equal(dirty.out[:, :N - 2], clean.out[:, :N - 2]), what
+        assert torch.equal(dirty.lse[:, :N - 2], clean.lse[:, :N - 2]), what
+        assert not torch.equal(dirty.lse[:, N - 2:], clean.lse[:, N - 2:])
