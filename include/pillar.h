@@ -320,7 +320,7 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  *              (first < 0) commits nothing.
  *   scores     the statistic of the verification, or NULL: its entries move along.
  *   new_lens   device [B] int32, receives first + the length of the path; no part of
- *              it may be kv->seq_lens.
+ *              it may be kv->seq_lens, tree_sizes, path or path_lens (PILLAR_EINVAL).
  * WRITES into the pools and, for fp8, into k_scale and v_scale: a page that
  * receives rows gets the largest scale that any of its rows up to the new length
  * had, and those rows are rounded anew to codes of that scale (at most half a

@@ -544,9 +544,11 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
   if (!path || !path_lens || !new_lens || max_path < 1) return PILLAR_EINVAL;
   if (max_path > tree_nodes_max()) return PILLAR_EUNSUPPORTED;
   if (scores && score_stride < kv->max_seq_len) return PILLAR_EINVAL;
-  // the heads of a request read its length while one of them writes the new one
+  // the heads of a request read its length, tree and path while one of them writes the new length
   const uint64_t span = static_cast<uint64_t>(kv->batch) * 4;
-  if (overlap(kv->seq_lens, span, new_lens, span)) return PILLAR_EINVAL;
+  if (overlap(kv->seq_lens, span, new_lens, span) || overlap(path_lens, span, new_lens, span) || overlap(path, span * max_path, new_lens, span) ||
+      (tree_sizes && overlap(tree_sizes, span, new_lens, span)))
+    return PILLAR_EINVAL;
   if (!rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
   CommitArgs a;
   a.kv = make_view(kv);
