@@ -357,7 +357,7 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
  *              whatever is equal is resolved towards the lower slot.  (Weights are
  *              >= 0; one that is negative or NaN counts as 0.)
  *   new_lens   device [B] int32, receives K'.  May be kv->seq_lens, old_lens or
- *              budgets itself, but must not overlap them in part.
+ *              budgets itself, but must not overlap them in part (PILLAR_EINVAL).
  * Attention does not depend on the order of the rows, so the tokens that stay are
  * not closed up: those in slots below K' stay where they are and those beyond move
  * into the freed slots below K', the i-th into the i-th, K, V, weight and position

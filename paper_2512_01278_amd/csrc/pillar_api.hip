@@ -577,6 +577,10 @@ int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_st
   if (!old_lens || !budgets || !weights || !positions || !new_lens) return PILLAR_EINVAL;
   if (!(decay >= 0.f) || !(decay < 1e30f) || sink_tokens < 0 || recent_tokens < 0) return PILLAR_EINVAL;
   if (state_stride < kv->max_seq_len || (scores && score_stride < kv->max_seq_len)) return PILLAR_EINVAL;
+  // in place or apart: else a request's new length would be another's length or budget
+  const uint64_t span = static_cast<uint64_t>(kv->batch) * 4;
+  for (const int32_t* p : {kv->seq_lens, old_lens, budgets})
+    if (p != new_lens && overlap(p, span, new_lens, span)) return PILLAR_EINVAL;
   if (!fits_a_grid(kv) || !rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
   EvictArgs a;
   a.kv = make_view(kv);

@@ -26,3 +26,16 @@ def test_commit_writes_over_nothing_that_it_reads(lib, batch, M):  # noqa: F811
     for address, span in ((seq, mine), (sizes, mine), (lens, mine), (path, mine * M)):
         for place in around(address, span, mine):
             assert tc(place) == pb.PILLAR_EINVAL, (hex(address), place - address)
+
+
+@pytest.mark.parametrize("batch", [2, 3, 64])
+def test_eviction_writes_over_whole_arrays_or_none(lib, batch):  # noqa: F811
+    """New lengths may replace the lengths, the old lengths or the budgets, but not those of other requests."""
+    old, budgets, now, seq = APART[:4]
+    kv = good_kv(batch=batch, seq_lens=seq)
+
+    def ev(now):
+        return lib.pillar_evict_kv(C.byref(kv), FAKE, 1024, 0.5, old, budgets, 4, 64, FAKE, FAKE, 1024, now, FAKE, 1 << 40, None)
+    for address in (old, budgets, seq):
+        for step in (4, 4 * batch - 4, 2 * batch):
+            assert ev(address + step) == ev(address - step) == pb.PILLAR_EINVAL, (hex(address), step)
