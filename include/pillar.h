@@ -305,8 +305,10 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  * run on bf16 matrix instructions (P is rounded to bf16), if q, out, the pools and
  * their strides are multiples of 16 bytes; everything else, and with
  * PILLAR_FLAG_GENERIC_KERNELS everything, on fp32 ones.  lse and scores carry
- * fp32 rounding only.  fp8 scales of what is seen are finite and not negative (a
- * v_scale below 2^-100 counts as that).  PILLAR_FLAG_EXACT_SCORES changes nothing here.
+ * fp32 rounding only.  fp8 scales of what is seen are finite and not negative; on bf16
+ * instructions a v_scale below 2^-80 counts as that, and what lse lacks, if anything,
+ * are probabilities below 2^-46 times the largest v_scale that the row sees.
+ * PILLAR_FLAG_EXACT_SCORES changes nothing here.
  * workspace: pillar_tree_workspace_bytes() (0: invalid arguments), enough for any
  * smaller batch, max_seq_len and N too.
  *

@@ -24,6 +24,10 @@ namespace pillar {
 namespace {
 
 constexpr int kTreeNodes = 64;
+// What a smaller v_scale (that of a page of zeros) counts as: far enough below any other for its rows to add nothing to O, and a token's share of l, which passes
+// through an exponential with v_scale in its exponent, is flushed (at 2^-126) only from 2^-46 of the largest scale on.  (2^-100: from 2^-26, 2000 tokens of
+// 2^-20 beside a page of scale 2^12 were missing from l.)  2^8 / kLeastScale times all tokens there may be stays below 2^128.
+constexpr float kLeastScale = 0x1p-80f;
 
 struct TreeParams {
   KvView kv;
@@ -385,7 +389,7 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
       // one token dominates off by 2^-8 (64 fp8 requests, out against 64 bits: 0.0024 of its norm, now 0.0018 of which 0.0017 is out's own
       // rounding; 611 / 637 us).
       if (C::kScales && tid < TS) {
-        const float log_vs = __builtin_amdgcn_logf(c.vs < 0x1p-100f ? 0x1p-100f : c.vs);      // (zero: as small as l can carry)
+        const float log_vs = __builtin_amdgcn_logf(c.vs < kLeastScale ? kLeastScale : c.vs);
         s_ks[tid] = c.ks * scale2;
         s_log_vs[tid] = log_vs;
         s_inv_vs[tid] = fast_exp2(-log_vs);              // (of the rounded logarithm: l is exact to fp32)
