@@ -385,9 +385,9 @@ __global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void tree_pass(Tre
           park_v(c.v[i], c.v_scale(i), s, c.row(i), c.piece, tail);
         }
       }
-      // With v_scale in the exponent the weightiest p v_scale of a tile is 1, which bf16 has exactly; as a factor on P it left the weight of a row that
-      // one token dominates off by 2^-8 (64 fp8 requests, out against 64 bits: 0.0024 of its norm, now 0.0018 of which 0.0017 is out's own
-      // rounding; 611 / 637 us).
+      // With v_scale in the exponent p v_scale is 1, which bf16 has exactly, for the token that set a row's running maximum; as a factor on P it left the
+      // weight of a row that one token dominates off by 2^-8 (64 fp8 requests, out against 64 bits: 0.0024 of its norm, now 0.0018 of which
+      // 0.0017 is out's own rounding; 611 / 637 us).  A later token that exceeds the maximum by up to 8 does not move it, and is rounded like any other.
       if (C::kScales && tid < TS) {
         const float log_vs = __builtin_amdgcn_logf(c.vs < kLeastScale ? kLeastScale : c.vs);
         s_ks[tid] = c.ks * scale2;
