@@ -352,12 +352,19 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
  *              they were: clear them where there may be one.)
  *   positions  device [B][Hkv][state_stride] int32, in and out: the place of each
  *              cached token in the text.  New tokens are numbered on from the
- *              largest of the old ones (from 0 where there is none).
+ *              largest number that the head still holds (from 0 where there is
+ *              none), which is their place as long as the newest token has never
+ *              been evicted: recent_tokens >= 1 and budgets of sink_tokens +
+ *              recent_tokens or more see to that.  Where it may go, numbers would
+ *              be given twice; there the caller writes the positions of the new
+ *              tokens itself, and weights of 0 (which become their scores), and
+ *              passes old_lens = kv->seq_lens.
  *   budgets    device [B]: K' = min(budgets[b], L) tokens of each head stay:
- *              first those with a position below sink_tokens or among the
- *              recent_tokens largest numbers, then those of largest weight;
- *              whatever is equal is resolved towards the lower slot.  (Weights are
- *              >= 0; one that is negative or NaN counts as 0.)
+ *              first the protected ones, with a position below sink_tokens or
+ *              less than recent_tokens below the largest (a window of numbers: it
+ *              has fewer tokens where some of them went before), then those of
+ *              largest weight; whatever is equal is resolved towards the lower
+ *              slot.  (Weights are >= 0; one that is negative or NaN counts as 0.)
  *   new_lens   device [B] int32, receives K'.  May be kv->seq_lens, old_lens or
  *              budgets itself, but must not overlap them in part (PILLAR_EINVAL).
  * Attention does not depend on the order of the rows, so the tokens that stay are
