@@ -376,7 +376,11 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
  * pillar_tree_commit does.  No page may belong to two requests.
  * state_stride >= max_seq_len; 0 <= decay < 1e30; pools and strides in multiples
  * of 16 bytes, else PILLAR_EUNSUPPORTED.  (Rows leave their order: queries of
- * a later verification must follow the cached tokens, as they do when appended.)
+ * a later verification must follow the cached tokens, as they do when appended.
+ * The index calls go by slots: pillar_window_indices names the first and last slots,
+ * which after an eviction are not the first and last tokens of the text.  A list of
+ * those is to be made from `positions`, for each KV head.  Top-K lists, and
+ * pillar_extend_indices for tokens appended since, name slots as ever.)
  * workspace: pillar_evict_workspace_bytes() (0: invalid description). */
 size_t pillar_evict_workspace_bytes(const pillar_kv_t* kv);
 int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_stride, float decay,
