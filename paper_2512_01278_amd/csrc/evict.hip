@@ -189,10 +189,27 @@ __device__ __forceinline__ void recode_page(const KvView& kv, const RowPlace& at
   }
 }
 
+// The pages of a (request, head), LANES lanes to each, so many side by side in each of the `workers` wavefronts.
+template <int LANES, typename Hole, typename Source>
+__device__ __forceinline__ void recode_all(const KvView& kv, const RowPlace& at, int g, int keep, int pages, const float (&edge_scale)[2], int moves, Hole hole, Source source,
+                                           int me, int workers) {
+  for (int p = me * (64 / LANES) + (threadIdx.x & 63) / LANES; p < pages; p += workers * (64 / LANES)) {
+    int lo = 0, hi = moves;                              // the page's first hole
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (hole(mid) < p << at.shift) lo = mid + 1;
+      else hi = mid;
+    }
+    if (lo < moves && hole(lo) >> at.shift == p) recode_page<LANES>(kv, at, g, keep, edge_scale, moves, hole, source, lo);
+  }
+}
+
 // Worker `me` of `workers` wavefronts.  A page is a chain of six loads and little else.  Where there are fewer holes than pages (a step at the budget:
 // a few rows in as many pages) the holes are dealt out, a wavefront to each, which has a page of 16 rows in one turn; else the
-// pages, sixteen lanes to each, four chains side by side.  64 requests, budget 4096, five new tokens: holes to 16 lanes 67 us, to wavefronts
-// 35; 32 prompts of 8 K: pages to wavefronts 110, to 16 lanes 95.
+// pages, sixteen lanes to each, four chains side by side, or from 32 rows on a wavefront, as the rows to write anew are what takes time.  64 requests,
+// budget 4096, five new tokens: holes to 16 lanes 67 us, to wavefronts 35.  32 prompts of 8 K whose pages have scales of their own, pages of 4, 8, 16,
+// 32, 64, 128 rows to 16 lanes 178, 166, 160, 166, 241, 372, to wavefronts 327, 203, 176, 162, 154, 163; 64 of 4 K 231, 211, 214, 222, 351, 361 and
+// 412, 251, 218, 188, 182, 207; 16 of 32 K, pages of 16, 32, 64, 176, 277, 490 and 211, 190, 178.
 template <typename Hole, typename Source>
 __device__ __forceinline__ void recode_pages(const KvView& kv, const RowPlace& at, int g, int keep, const float (&edge_scale)[2], int moves, Hole hole, Source source,
                                              int me, int workers) {
@@ -200,17 +217,10 @@ __device__ __forceinline__ void recode_pages(const KvView& kv, const RowPlace& a
   if (moves < pages) {
     for (int h = me; h < moves; h += workers)
       if (h == 0 || hole(h) >> at.shift != hole(h - 1) >> at.shift) recode_page<64>(kv, at, g, keep, edge_scale, moves, hole, source, h);
-    return;
-  }
-  constexpr int kLanes = 16;
-  for (int p = me * (64 / kLanes) + (threadIdx.x & 63) / kLanes; p < pages; p += workers * (64 / kLanes)) {
-    int lo = 0, hi = moves;                              // the page's first hole
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (hole(mid) < p << at.shift) lo = mid + 1;
-      else hi = mid;
-    }
-    if (lo < moves && hole(lo) >> at.shift == p) recode_page<kLanes>(kv, at, g, keep, edge_scale, moves, hole, source, lo);
+  } else if (at.mask < 31) {
+    recode_all<16>(kv, at, g, keep, pages, edge_scale, moves, hole, source, me, workers);
+  } else {
+    recode_all<64>(kv, at, g, keep, pages, edge_scale, moves, hole, source, me, workers);
   }
 }
 
