@@ -100,6 +100,17 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// running sum over the lanes
+__device__ __forceinline__ int wave_inclusive(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8: within rows of 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);    // row_bcast 15: a row's sum into the next, rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // row_bcast 31: of the first two into the others
+  return v;
+}
+
 // element offset of (token t of request b, KV head g) in a pool, and its page
 __device__ __forceinline__ int64_t row_offset(const KvView& kv, int b, int g, int t, int* page_out) {
   const int page = kv.block_table[static_cast<int64_t>(b) * kv.block_table_stride + (t >> kv.page_shift)];

@@ -46,17 +46,6 @@ __device__ __forceinline__ float accumulate(float weight, float decay, float sco
   return weight * decay + score;
 }
 
-// running sum over the lanes of a wavefront
-__device__ __forceinline__ int lanes_inclusive(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);    // row_bcast 15
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // row_bcast 31
-  return v;
-}
-
 // Rows are read several at a time before any is written: the compiler cannot know that no load depends on a store before it.
 constexpr int kBatch = 2;
 
@@ -343,7 +332,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 1 : NQ <= 2 && !FP8 ? 8 :
         const int bin = static_cast<int>(bins) - 1 - (tid * per + i);
         if (i < per && bin >= 0) mine += hist[pass][bin];
       }
-      int upto = lanes_inclusive(mine);
+      int upto = wave_inclusive(mine);
       if (lane == 63) s_sum[wave] = upto;
       __syncthreads();
       for (int i = 0; i < wave; ++i) upto += s_sum[i];
@@ -375,13 +364,13 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 1 : NQ <= 2 && !FP8 ? 8 :
   auto ranks = [&](const uint32_t (&flags)[NQ], int (&rank)[NQ], int base, int* totals) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const int mine = __popc(flags[q]), upto = lanes_inclusive(mine);
+      const int mine = __popc(flags[q]), upto = wave_inclusive(mine);
       if (lane == 63) totals[q * kWaves + wave] = upto;
       rank[q] = upto - mine;
     }
     __syncthreads();
     int x0 = lane < NQ * kWaves ? totals[lane] : 0, x1 = 64 + lane < NQ * kWaves ? totals[64 + lane] : 0;
-    const int i0 = lanes_inclusive(x0), half = __builtin_amdgcn_readlane(i0, 63), i1 = lanes_inclusive(x1) + half;
+    const int i0 = wave_inclusive(x0), half = __builtin_amdgcn_readlane(i0, 63), i1 = wave_inclusive(x1) + half;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int e = q * kWaves + wave;

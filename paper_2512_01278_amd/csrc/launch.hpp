@@ -11,6 +11,13 @@ namespace pillar {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Rows of the pools can be read and written 16 bytes at a time: bases and strides are multiples of that.
+inline bool rows_aligned(const KvView& kv, int kv_dtype) {
+  const int64_t per = kv_dtype == PILLAR_F32 ? 4 : kv_dtype == PILLAR_BF16 ? 8 : 16;       // elements per 16 bytes
+  return kv.stride_page % per == 0 && kv.stride_head % per == 0 && kv.stride_slot % per == 0 &&
+         ((reinterpret_cast<uintptr_t>(kv.k_pool) | reinterpret_cast<uintptr_t>(kv.v_pool)) & 15u) == 0;
+}
+
 // Brackets one kernel launch with HIP events when profiling is switched on.
 struct KernelTimer {
   KernelTimer(const char* name, hipStream_t stream);

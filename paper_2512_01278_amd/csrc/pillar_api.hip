@@ -125,13 +125,6 @@ int check_workspace(const void* ws, size_t have, size_t need) {
   return PILLAR_OK;
 }
 
-// rows are copied in 16-byte pieces: pools and strides are multiples of that
-bool rows_in_pieces(const pillar_kv_t* kv) {
-  const int64_t esz = kv->kv_dtype == PILLAR_F32 ? 4 : kv->kv_dtype == PILLAR_BF16 ? 2 : 1;
-  return (kv->stride_page * esz) % 16 == 0 && (kv->stride_head * esz) % 16 == 0 && (kv->stride_slot * esz) % 16 == 0 &&
-         ((reinterpret_cast<uintptr_t>(kv->k_pool) | reinterpret_cast<uintptr_t>(kv->v_pool)) & 15u) == 0;
-}
-
 bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
   const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + b_bytes && y < x + a_bytes;
@@ -549,9 +542,9 @@ int pillar_tree_commit(const pillar_kv_t* kv, const int32_t* tree_sizes, int32_t
   if (overlap(kv->seq_lens, span, new_lens, span) || overlap(path_lens, span, new_lens, span) || overlap(path, span * max_path, new_lens, span) ||
       (tree_sizes && overlap(tree_sizes, span, new_lens, span)))
     return PILLAR_EINVAL;
-  if (!rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
   CommitArgs a;
   a.kv = make_view(kv);
+  if (!rows_aligned(a.kv, kv->kv_dtype)) return PILLAR_EUNSUPPORTED;
   a.tree_sizes = tree_sizes;
   a.max_nodes = max_nodes;
   a.max_path = max_path;
@@ -581,9 +574,9 @@ int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_st
   const uint64_t span = static_cast<uint64_t>(kv->batch) * 4;
   for (const int32_t* p : {kv->seq_lens, old_lens, budgets})
     if (p != new_lens && overlap(p, span, new_lens, span)) return PILLAR_EINVAL;
-  if (!fits_a_grid(kv) || !rows_in_pieces(kv)) return PILLAR_EUNSUPPORTED;
   EvictArgs a;
   a.kv = make_view(kv);
+  if (!fits_a_grid(kv) || !rows_aligned(a.kv, kv->kv_dtype)) return PILLAR_EUNSUPPORTED;
   rc = check_workspace(workspace, workspace_bytes, evict_workspace(a.kv));
   if (rc != PILLAR_OK) return rc;
   a.scores = scores;

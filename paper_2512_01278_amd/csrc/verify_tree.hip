@@ -97,17 +97,6 @@ struct Ranges {
   }
 };
 
-// running sum over the lanes of a wavefront
-__device__ __forceinline__ int wave_inclusive(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr 1, 2, 4, 8: within rows of 16 lanes
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);    // row_bcast 15: a row's sum into the next, rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // row_bcast 31: of the first two into the others
-  return v;
-}
-
 // What a workgroup finds out about its share of the work, every wavefront for itself: 64 requests at a time, a request per lane.
 struct Share {
   int w, u0, u1;               // its range, first unit and past the last
@@ -815,12 +804,6 @@ TreeWs carve(const KvView& kv, int max_nodes, const TreePlan& p) {
 bool strides_fit(const KvView& kv, int kv_dtype) {
   const int64_t most = (int64_t{1} << 32) / (kv_dtype == PILLAR_BF16 ? 2 : 1) - 1;
   return kv.stride_page <= most && kv.stride_slot <= most;
-}
-
-bool rows_aligned(const KvView& kv, int kv_dtype) {
-  const int64_t per = kv_dtype == PILLAR_F32 ? 4 : kv_dtype == PILLAR_BF16 ? 8 : 16;       // elements per 16 bytes
-  return kv.stride_page % per == 0 && kv.stride_head % per == 0 && kv.stride_slot % per == 0 &&
-         ((reinterpret_cast<uintptr_t>(kv.k_pool) | reinterpret_cast<uintptr_t>(kv.v_pool)) & 15u) == 0;
 }
 
 template <typename C>
