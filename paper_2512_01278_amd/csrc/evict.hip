@@ -536,10 +536,12 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   const int esz = a.kv_dtype == PILLAR_F32 ? 4 : a.kv_dtype == PILLAR_BF16 ? 2 : 1;
   const bool wide = a.state_stride % 4 == 0 && (!a.scores || a.score_stride % 4 == 0) &&
                     ((reinterpret_cast<uintptr_t>(a.weights) | reinterpret_cast<uintptr_t>(a.positions) | reinterpret_cast<uintptr_t>(a.scores)) & 15u) == 0;
-  // One launch, in which the workgroup that selects moves its rows too, where that fills the chip or the rows are short; else few workgroups would
-  // move many rows.  Two / one: 64 requests, 5 of 4101 tokens, 22 / 18 us, one, 2 of 2050 15 / 13, 2048 of 4096 16 / 13, 31, 16 of 8016 20 / 17;
-  // fp8: 8, 4 of 4004 25 / 16, one, 2048 of 4096 37 / 44; one, 20000 of 21000 30 / 37.  (Not where the new lengths replace what the
-  // workgroups of other heads read.)
+  // One launch, in which the workgroup that selects moves its rows too, where that fills the chip or the rows are short.  The host does not know how many rows
+  // will move, and a step at the budget moves few.  Two / one, on caches restored before each pass (us): steps, one request, 2 of 2050 11.4 / 9.6, 8, 4
+  // of 4004 14.4 / 11.9, 31, 16 of 8016 22 / 19, 64, 5 of 4101 24 / 20; fp8 17 / 15.5, 30 / 18, 37 / 30.5, 47 / 40.  The first eviction of a prompt
+  // loses by it where there are few pairs: one of 4096 to 2048 14.6 / 24, fp8 65 / 106, 8 of 8192 36 / 75, 124 / 133, 31 105 / 101, 152 / 158; steps are
+  // hundreds to a prompt.  Beyond 8192 tokens it would lose more than steps gain: one of 32 K to 4096 43 / 111, fp8 122 / 259, one of
+  // 21000 to 20000 41 / 50, 56 / 358; steps of 16000 33 / 31, 45 / 39.  (Not where the new lengths replace what the workgroups of other heads read.)
   auto apart = [&](const int32_t* p) { return a.new_lens + a.kv.batch <= p || p + a.kv.batch <= a.new_lens; };
   const bool moves_rows = (pairs >= num_cus() || a.kv.max_seq_len <= 8192) && apart(a.kv.seq_lens) && apart(a.old_lens) && apart(a.budgets);
   const bool fp8 = a.kv_dtype == PILLAR_FP8_E4M3;
