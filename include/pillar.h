@@ -293,6 +293,9 @@ int pillar_extend_indices(int32_t* indices, int32_t* counts, const int32_t* firs
  *              nodes will do, and bits from tree_sizes[b] on are ignored).  Every
  *              node attends to all tokens before the tree.  A chain is
  *              visible[b][i] = 2^(i+1) - 1, plain decoding N = 1 and a word of 1.
+ *              (With the statistic, K is read twice here: chains of up to about 40 rows
+ *              per KV head, and single tokens, are faster through pillar_verify_attn,
+ *              whose scores have 11 bits.)
  *   out, lse, scores, score_stride: as in pillar_verify_attn, the statistic being
  *              the mean over the tree_sizes[b]*G rows; no part of out may be q
  *              (PILLAR_EINVAL).  Slots from tree_sizes[b] on and scores from

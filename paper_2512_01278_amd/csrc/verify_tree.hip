@@ -13,7 +13,10 @@
 //                device need no plan on the host.  A stretch of one tile that a range does not hold whole leaves a partial (m, l, O).
 //   tree_merge   joins the partials.
 //   tree_scores  (with scores) K once more against the final log-sum-exp, summed over the rows.  With n G rows a stash of P would be 2 n G
-//                bytes a token written and read where K's second read is 2 D: at 64 and more rows the read is less.
+//                bytes a token written and read where K's second read is 2 D: at 64 and more rows the read is less.  With fewer it is not: chains have
+//                the calls of verify_range.hip, which stash (in 11 bits).  64 requests of 8192 tokens with the statistic, 4 heads to a KV head, this /
+//                those: one node 522 / 391 us, 4 540 / 441, 8 536 / 515, 12 562 / 582, 16 554 / 641; fp8 318 / 218, 327 / 265, 323 / 322, 425 /
+//                361, 422 / 453.  A tree of few rows takes the second read all the same, and has fp32 scores.
 #include <algorithm>
 
 #include "host_rules.hpp"
