@@ -195,10 +195,10 @@ __device__ __forceinline__ void recode_all(const KvView& kv, const RowPlace& at,
 
 // Worker `me` of `workers` wavefronts.  A page is a chain of six loads and little else.  Where there are fewer holes than pages (a step at the budget:
 // a few rows in as many pages) the holes are dealt out, a wavefront to each, which has a page of 16 rows in one turn; else the
-// pages, sixteen lanes to each, four chains side by side, or from 32 rows on a wavefront, as the rows to write anew are what takes time.  64 requests,
-// budget 4096, five new tokens: holes to 16 lanes 67 us, to wavefronts 35.  32 prompts of 8 K whose pages have scales of their own, pages of 4, 8, 16,
-// 32, 64, 128 rows to 16 lanes 178, 166, 160, 166, 241, 372, to wavefronts 327, 203, 176, 162, 154, 163; 64 of 4 K 231, 211, 214, 222, 351, 361 and
-// 412, 251, 218, 188, 182, 207; 16 of 32 K, pages of 16, 32, 64, 176, 277, 490 and 211, 190, 178.
+// pages, sixteen lanes to each, four chains side by side, or from 32 rows on a wavefront, as the rows to write anew are what takes time.  Both sides on caches
+// restored before each pass, whose pages have scales of their own (us): 64 requests, budget 4096, five new tokens, holes to 16 lanes 50, to wavefronts 40; 32
+// prompts of 8 K, pages of 4, 8, 16, 32, 64, 128 rows to 16 lanes 178, 166, 160, 166, 241, 372, to wavefronts 327, 203, 176, 162, 154, 163; 64 of 4 K
+// 231, 211, 214, 222, 351, 361 and 412, 251, 218, 188, 182, 207; 16 of 32 K, pages of 16, 32, 64, 176, 277, 490 and 211, 190, 178.
 template <typename Hole, typename Source>
 __device__ __forceinline__ void recode_pages(const KvView& kv, const RowPlace& at, int g, int keep, const float (&edge_scale)[2], int moves, Hole hole, Source source,
                                              int me, int workers) {
