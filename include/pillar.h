@@ -391,6 +391,104 @@ int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_st
                     int32_t recent_tokens, float* weights, int32_t* positions, int64_t state_stride,
                     int32_t* new_lens, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- Rotary positions, and new tokens into the cache ---------------------
+ *
+ * A rotation turns pair i (of rotary_dim / 2) of a head by the angle position * frequencies[i], and multiplies it by `amplitude`:
+ *   y1 = amplitude * (x1 cos - x2 sin),  y2 = amplitude * (x2 cos + x1 sin)
+ * The pair is (dim i, dim i + rotary_dim/2), or with PILLAR_ROPE_INTERLEAVED (dim 2i, dim 2i + 1).  Dims from rotary_dim on stay as they are.
+ * Angles are worked out in 64 bits (positions of any size keep their precision), the rest in fp32, with one rounding to the output's type.
+ * Positions may be negative: the rotation by -position undoes one by position (and its amplitude, if the second one has 1 / amplitude).
+ * frequencies: device [rotary_dim / 2] double, 8-byte aligned; rotary_dim even, 2..head_dim. */
+typedef enum { PILLAR_ROPE_HALVES = 0, PILLAR_ROPE_INTERLEAVED = 1 } pillar_rope_layout;
+typedef struct {
+  int32_t rotary_dim;
+  int32_t layout;              /* pillar_rope_layout */
+  float   amplitude;           /* finite; 1 unless the scaling says otherwise */
+  int32_t reserved;            /* 0 */
+  const double* frequencies;   /* device */
+} pillar_rope_t;
+
+/* Frequencies of a model, host arithmetic: frequencies[i] = base^(-2 i / rotary_dim), changed for contexts that are `factor` times the
+ * original_len positions that it was trained on:
+ *   NONE    as they are (factor, original_len, fast and slow are not looked at)
+ *   LINEAR  all divided by factor
+ *   BASE    base * factor^(r / (r - 2)) instead of base (r = rotary_dim; r = 2 counts as r / 1): the lowest frequency is divided by about factor
+ *   RAMP    pairs of more than `fast` turns over original_len stay, those of fewer than `slow` are divided by factor, linear in i between; amplitude
+ *           0.1 ln(factor) + 1.  The two ends are i = r ln(original_len / (2 pi turns)) / (2 ln base), rounded down and up.
+ *   BANDS   the same two ends, linear in the number of turns between; amplitude 1
+ * frequencies: HOST [rotary_dim / 2], to be copied to the device once; amplitude: host, receives the factor for pillar_rope_t. */
+typedef enum { PILLAR_ROPE_NONE = 0, PILLAR_ROPE_LINEAR = 1, PILLAR_ROPE_BASE = 2, PILLAR_ROPE_RAMP = 3, PILLAR_ROPE_BANDS = 4 } pillar_rope_scaling;
+int pillar_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, int32_t original_len,
+                            double fast, double slow, double* frequencies, float* amplitude);
+
+/* Rows of heads by themselves (queries apart from their keys, keys that get other positions).
+ *   x    device [tokens][num_heads][head_dim] of `dtype` (PILLAR_F32 | PILLAR_BF16), token t at element t * x_stride (x_stride >= num_heads *
+ *        head_dim: rows of a fused projection will do), heads dense within; out likewise.
+ *   positions  device [tokens] int32.
+ * out may be x itself with the same stride; else the two spans must not overlap (PILLAR_EINVAL).  head_dim 2..512, even. */
+int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_heads, int32_t head_dim, int32_t dtype,
+                  const int32_t* positions, const pillar_rope_t* rope, void* out, int64_t out_stride, void* hip_stream);
+
+/* The newest tokens of every request: queries and keys are rotated, keys and values go into their pages (append, then attend: seq_lens
+ * already counts them).  Rows are packed: request b has rows starts[b] .. starts[b+1]-1, and row i of its n is token seq_lens[b] - n + i.
+ *   starts      device [B+1] int32, ascending, 0 <= starts[b] <= total_rows, at most max_new rows to a request; NULL: max_new rows each
+ *               (total_rows = B * max_new).  A request may have none.  Rows from starts[B] on are neither read nor written.
+ *   rope        NULL: nothing is rotated (q is copied).
+ *   positions   device [total_rows] int32 for the rotation, or NULL: the number of the token in the cache, seq_lens[b] - n + i.  (After an
+ *               eviction, and for the nodes of a tree, that is not the place in the text.)
+ *   q, q_out    [total_rows][Hq][D] q_dtype, q_out dense, row t of q at element t * q_stride; both NULL: no queries.  q_out may be q itself
+ *               if that is dense too, and must not overlap q, k_new or v_new otherwise (PILLAR_EINVAL).
+ *   k_new, v_new  [total_rows][Hkv][D] q_dtype, row t at element t * k_stride, v_stride.
+ * The cache may have any of its types: values are rounded once, to nearest even, from the fp32 result.  WRITES into the pools and, for fp8,
+ * into k_scale and v_scale: a page gets the largest scale of its older tokens' (those before the new ones; their codes are rounded anew where it
+ * grew, as by pillar_tree_commit) and what the new ones need, max |finite new value| / 448, or 0 where that maximum is below 2^-90; codes are
+ * those nearest to value * (1 / scale), infinities becoming the largest code (NaN in a page of scale 0), NaN staying NaN.  A page without older
+ * tokens takes the new ones' scale alone.
+ * Tokens whose number would be negative are skipped (their queries are rotated all the same).  No page that receives rows may belong to
+ * two requests.  Bases and strides of pools, q, k_new, v_new and q_out in multiples of 16 bytes, else PILLAR_EUNSUPPORTED. */
+int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, const int32_t* starts, int32_t total_rows, int32_t max_new,
+                          const int32_t* positions, const void* q, int64_t q_stride, void* q_out,
+                          const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* hip_stream);
+
+/* ---- Attention of new tokens -------------------------------------------
+ *
+ * Causal attention of any number of new tokens per request over its whole context: prompts, chunks of them, and single tokens beside
+ * them.  Rows are packed as in pillar_append_rotated, whose tokens they are: row i of request b's n attends to tokens 0 .. seq_lens[b]-n+i.
+ *   q, out  [total_rows][Hq][D] q_dtype, dense; no part of out may be q (PILLAR_EINVAL).
+ *   lse     [total_rows][Hq] fp32 natural-log-sum-exp of the logits, or NULL.
+ * A row that sees no token (its number is negative, or the request has no token) gets out = 0 and lse = -inf.  What a row does not see has no
+ * influence on it, whatever the cache holds there.  Every shape that pillar_kv_t can describe, group sizes up to 16.  bf16 queries with a bf16
+ * or fp8 cache run on bf16 matrix instructions (P is rounded to bf16), if q, out, the pools and their strides are multiples of 16 bytes;
+ * everything else, and with PILLAR_FLAG_GENERIC_KERNELS everything, on fp32 ones.  fp8 scales of what is seen are finite and not negative, and
+ * a v_scale below 2^-80 counts as in pillar_verify_tree.  PILLAR_FLAG_EXACT_SCORES changes nothing here.  (A few tokens per request that
+ * also want the statistic: pillar_verify_attn; trees: pillar_verify_tree.)
+ * workspace: pillar_prompt_workspace_bytes() (0: invalid arguments), enough for any smaller batch, total_rows, max_new and max_seq_len too. */
+size_t pillar_prompt_workspace_bytes(const pillar_kv_t* kv, int32_t total_rows, int32_t max_new);
+int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* starts, int32_t total_rows, int32_t max_new,
+                       void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- What the logits say about given tokens ------------------------------
+ *
+ * Rows of logits x, one per verified position or node: with z = scale * x,
+ *   lse[r]            = log sum_v exp(z[v])
+ *   logprobs[r][j]    = z[tokens[r][j]] - lse[r]
+ *   entropy[r]        = -sum_v p[v] log p[v],  p = exp(z - lse)                      (natural units throughout)
+ *   top_ids[r][j], top_logprobs[r][j], j < top: the tokens of largest logit, in descending order, equal ones by ascending id, and their log
+ *                       probabilities; where vocab < top the rest is -1 and -inf.
+ *   logits     device [rows][vocab] of `dtype` (PILLAR_F32 | PILLAR_BF16), row r at element r * row_stride (>= vocab); any alignment.
+ *   scale      one over the temperature; 0 < scale < 1e30.
+ *   tokens     device [rows][num_tokens] int32, or NULL with num_tokens 0; an entry outside 0..vocab-1 (a missing child, say) gets -inf.
+ *   lse, entropy: device [rows] fp32, each may be NULL.  top 0..64; top_ids and top_logprobs NULL exactly if top is 0.
+ * Logits of -inf (masked tokens) have probability 0 and add nothing to the entropy.  A row of nothing else: lse = -inf, all log probabilities
+ * -inf, entropy 0.  NaN makes the row's lse, log probabilities and entropy NaN, but it is nobody's alternative before all numbers, -inf among
+ * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Everything is summed in fp32 relative to the row's maximum.
+ * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments). */
+size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
+int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, float scale,
+                          const int32_t* tokens, int32_t num_tokens, float* logprobs, float* lse, float* entropy,
+                          int32_t top, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,8 @@ DTYPE_CODE = {"f32": PILLAR_F32, "bf16": PILLAR_BF16, "fp8_e4m3": PILLAR_FP8_E4M
 EXPORTS = ("pillar_version", "pillar_status_string", "pillar_workspace_bytes", "pillar_verify_attn",
            "pillar_verify_select", "pillar_verify_hetero", "pillar_mixed_step", "pillar_select_topk", "pillar_sparse_decode", "pillar_sparse_decode_static", "pillar_window_indices",
            "pillar_extend_indices", "pillar_append_kv", "pillar_tree_workspace_bytes", "pillar_verify_tree", "pillar_tree_commit",
-           "pillar_evict_workspace_bytes", "pillar_evict_kv", "pillar_profile_enable", "pillar_profile_reset",
+           "pillar_evict_workspace_bytes", "pillar_evict_kv", "pillar_rope_frequencies", "pillar_rotate", "pillar_append_rotated",
+           "pillar_prompt_workspace_bytes", "pillar_prompt_attn", "pillar_logprobs_workspace_bytes", "pillar_token_logprobs", "pillar_profile_enable", "pillar_profile_reset",
            "pillar_profile_read", "pillar_set_option", "pillar_bench_read")
 
 
@@ -42,6 +43,11 @@ class pillar_kv_t(C.Structure):
         ("block_table", C.c_void_p), ("seq_lens", C.c_void_p),
         ("max_seq_len", C.c_int32), ("flags", C.c_int32),
     ]
+
+
+class pillar_rope_t(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
+                ("frequencies", C.c_void_p)]
 
 
 class pillar_kernel_time(C.Structure):
@@ -117,6 +123,25 @@ def load() -> C.CDLL:
     lib.pillar_evict_kv.restype = C.c_int
     lib.pillar_evict_kv.argtypes = [C.POINTER(pillar_kv_t), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                     C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.pillar_rope_frequencies.restype = C.c_int
+    lib.pillar_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double,
+                                            C.POINTER(C.c_double), C.POINTER(C.c_float)]
+    lib.pillar_rotate.restype = C.c_int
+    lib.pillar_rotate.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.POINTER(pillar_rope_t),
+                                  C.c_void_p, C.c_int64, C.c_void_p]
+    lib.pillar_append_rotated.restype = C.c_int
+    lib.pillar_append_rotated.argtypes = [C.POINTER(pillar_kv_t), C.POINTER(pillar_rope_t), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
+                                          C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.pillar_prompt_workspace_bytes.restype = C.c_size_t
+    lib.pillar_prompt_workspace_bytes.argtypes = [C.POINTER(pillar_kv_t), C.c_int32, C.c_int32]
+    lib.pillar_prompt_attn.restype = C.c_int
+    lib.pillar_prompt_attn.argtypes = [C.POINTER(pillar_kv_t), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]
+    lib.pillar_logprobs_workspace_bytes.restype = C.c_size_t
+    lib.pillar_logprobs_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+    lib.pillar_token_logprobs.restype = C.c_int
+    lib.pillar_token_logprobs.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_int32, C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.pillar_bench_read.restype = C.c_int
     lib.pillar_bench_read.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
     lib.pillar_set_option.restype = C.c_int
@@ -396,6 +421,134 @@ def pillar_evict_kv(kv: KvCache, scores: Optional[torch.Tensor], decay: float, o
                                 _per_request(budgets, B, dev, "budgets"), sink_tokens, recent_tokens, weights_at, positions_at, state_stride,
                                 _per_request(new_lens, B, dev, "new_lens"), *_scratch(workspace, dev), _stream(stream))
     _check(rc, "pillar_evict_kv")
+
+
+# ---- rotary positions, new tokens, what their logits say ----
+ROPE_HALVES, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+_DTYPE_OF = {torch.float32: PILLAR_F32, torch.bfloat16: PILLAR_BF16}
+
+
+def pillar_rope_frequencies(rotary_dim: int, base: float, scaling: str = "none", factor: float = 1.0, original_len: int = 0,
+                            fast: float = 0.0, slow: float = 0.0) -> tuple:
+    """Frequencies (float64, on the CPU: copy them to the GPU once) and amplitude for a Rope."""
+    out, amplitude = torch.zeros(max(rotary_dim // 2, 1), dtype=torch.float64), C.c_float()
+    rc = load().pillar_rope_frequencies(rotary_dim, base, ROPE_SCALINGS[scaling], factor, original_len, fast, slow,
+                                        C.cast(out.data_ptr(), C.POINTER(C.c_double)), C.byref(amplitude))
+    _check(rc, "pillar_rope_frequencies")
+    return out, amplitude.value
+
+
+@dataclass
+class Rope:
+    """The tensor behind one pillar_rope_t."""
+    frequencies: torch.Tensor      # float64 [rotary_dim / 2], on the GPU
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+    def c_struct(self, dev: int) -> pillar_rope_t:
+        f = self.frequencies
+        if f.dtype is not torch.float64 or f.dim() != 1 or f.get_device() != dev or not f.is_contiguous():
+            _refuse(f, "frequencies", "float64 tensor [rotary_dim / 2]", dev)
+        return pillar_rope_t(2 * f.numel(), ROPE_INTERLEAVED if self.interleaved else ROPE_HALVES, self.amplitude, 0, f.data_ptr())
+
+
+def _current(t: torch.Tensor, what: str) -> int:
+    """The GPU of a tensor, which is the current one."""
+    dev = t.get_device()
+    if dev >= 0 and dev != torch.cuda.current_device():
+        raise ValueError(f"{what}: on cuda:{dev}, which is not the current device")
+    if dev < 0 and torch.cuda.is_available():
+        raise ValueError(f"{what}: in host memory")
+    return dev
+
+
+def _head_rows(t: Optional[torch.Tensor], dtype: torch.dtype, rows: Optional[int], heads: Optional[int], D: Optional[int], dev: int, what: str) -> tuple:
+    """Address and row stride of [rows][heads][D] whose heads are dense; the rows may lie apart."""
+    if t is None:
+        return None, 0
+    shape, strides = t.shape, t.stride()
+    fits = len(shape) == 3 and (rows is None or shape[0] == rows) and (heads is None or shape[1] == heads) and (D is None or shape[2] == D)
+    # (the stride of an axis of one says nothing)
+    dense = fits and (strides[2] == 1 or shape[2] == 1) and (strides[1] == shape[2] or shape[1] == 1)
+    if t.dtype is not dtype or t.get_device() != dev or not dense:
+        _refuse(t, what, f"{dtype} tensor [{rows or 'tokens'}, {heads or 'heads'}, {D or 'head_dim'}], dense but for its rows,", dev)
+    return t.data_ptr(), strides[0] if shape[0] > 1 else max(strides[0], shape[1] * shape[2])
+
+
+def pillar_rotate(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: torch.Tensor, stream=None) -> None:
+    dev = _current(x, "x")
+    if x.dtype not in _DTYPE_OF or x.dim() != 3:
+        _refuse(x, "x", "fp32 or bf16 tensor [tokens, heads, head_dim]", dev)
+    T, H, D = x.shape
+    x_at, x_stride = _head_rows(x, x.dtype, T, H, D, dev, "x")
+    out_at, out_stride = _head_rows(out, x.dtype, T, H, D, dev, "out")
+    r = rope.c_struct(dev)
+    rc = load().pillar_rotate(x_at, x_stride, T, H, D, _DTYPE_OF[x.dtype], _per_request(positions, T, dev, "positions"), C.byref(r), out_at, out_stride,
+                              _stream(stream))
+    _check(rc, "pillar_rotate")
+
+
+def pillar_append_rotated(kv: KvCache, rope: Optional[Rope], k_new: torch.Tensor, v_new: torch.Tensor, max_new: int,
+                          starts: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                          q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    s, dev = kv.c_struct(), _device(kv)
+    T, qt = k_new.shape[0], _Q_TORCH[kv.q_dtype]
+    k_at, k_stride = _head_rows(k_new, qt, T, s.num_kv_heads, s.head_dim, dev, "k_new")
+    v_at, v_stride = _head_rows(v_new, qt, T, s.num_kv_heads, s.head_dim, dev, "v_new")
+    q_at, q_stride = _head_rows(q, qt, T, s.num_q_heads, s.head_dim, dev, "q")
+    r = None if rope is None else C.byref(rope.c_struct(dev))
+    rc = load().pillar_append_rotated(C.byref(s), r, _per_request(starts, s.batch + 1, dev, "starts"), T, max_new,
+                                      _per_request(positions, T, dev, "positions"), q_at, q_stride,
+                                      _tensor(q_out, qt, (T, s.num_q_heads, s.head_dim), dev, "q_out"), k_at, k_stride, v_at, v_stride, _stream(stream))
+    _check(rc, "pillar_append_rotated")
+
+
+def pillar_prompt_workspace_bytes(kv: KvCache, total_rows: int, max_new: int) -> int:
+    s = kv.c_struct()
+    return int(load().pillar_prompt_workspace_bytes(C.byref(s), total_rows, max_new))
+
+
+def pillar_prompt_attn(kv: KvCache, q: torch.Tensor, max_new: int, out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor,
+                       starts: Optional[torch.Tensor] = None, stream=None) -> None:
+    s, dev = kv.c_struct(), _device(kv)
+    shape, qt = (q.shape[0], s.num_q_heads, s.head_dim), _Q_TORCH[kv.q_dtype]
+    rc = load().pillar_prompt_attn(C.byref(s), _tensor(q, qt, shape, dev, "q"), _per_request(starts, s.batch + 1, dev, "starts"), shape[0], max_new,
+                                   _tensor(out, qt, shape, dev, "out"), _tensor(lse, _F32, shape[:2], dev, "lse"), *_scratch(workspace, dev),
+                                   _stream(stream))
+    _check(rc, "pillar_prompt_attn")
+
+
+def pillar_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    return int(load().pillar_logprobs_workspace_bytes(rows, vocab, top))
+
+
+def pillar_token_logprobs(logits: torch.Tensor, workspace: torch.Tensor, tokens: Optional[torch.Tensor] = None, logprobs: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
+                          top_logprobs: Optional[torch.Tensor] = None, scale: float = 1.0, stream=None) -> None:
+    """logits: [rows, vocab], rows dense in themselves; tokens, logprobs: [rows, any number]; top_ids, top_logprobs: [rows, top]."""
+    dev = _current(logits, "logits")
+    if logits.dtype not in _DTYPE_OF or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse(logits, "logits", "fp32 or bf16 tensor [rows, vocab], dense but for its rows,", dev)
+    R, V = logits.shape
+    M, N = 0 if tokens is None else tokens.shape[-1], 0 if top_ids is None else top_ids.shape[-1]
+    if (tokens is None) != (logprobs is None) or (top_ids is None) != (top_logprobs is None):
+        raise ValueError("tokens and logprobs, top_ids and top_logprobs: both or neither are wanted")
+    some = lambda t, n, *rest: _tensor(t, *rest) if n else None
+    rc = load().pillar_token_logprobs(logits.data_ptr(), _DTYPE_OF[logits.dtype], R, V, logits.stride(0) if R > 1 else V, scale,
+                                      some(tokens, M, _I32, (R, M), dev, "tokens"), M, some(logprobs, M, _F32, (R, M), dev, "logprobs"),
+                                      _per_row(lse, R, dev, "lse"), _per_row(entropy, R, dev, "entropy"), N, some(top_ids, N, _I32, (R, N), dev, "top_ids"),
+                                      some(top_logprobs, N, _F32, (R, N), dev, "top_logprobs"), *_scratch(workspace, dev), _stream(stream))
+    _check(rc, "pillar_token_logprobs")
+
+
+def _per_row(t: Optional[torch.Tensor], n: int, dev: int, what: str) -> Optional[int]:
+    """fp32, one entry per row."""
+    if t is None:
+        return None
+    if t.dtype is not _F32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, what, f"fp32 tensor of {n}", dev)
+    return t.data_ptr()
 
 
 def pillar_bench_read(buf: torch.Tensor, n_chunks: int, chunk_bytes: int, order: Optional[torch.Tensor], blocks: int,

@@ -10,6 +10,7 @@ namespace pillar {
 
 constexpr int kWave = 64;
 constexpr int kMaxRows = 64;      // (k+1)*G rows of one KV head at most
+constexpr int kMostAlternatives = 64;   // of a row of logits
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 

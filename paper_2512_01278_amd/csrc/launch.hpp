@@ -165,6 +165,73 @@ hipError_t launch_tree_commit(const CommitArgs& a, hipStream_t s);
 size_t evict_workspace(const KvView& kv);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 
+// new tokens (rotate.hip, prompt_attn.hip) and their logits (logprobs.hip)
+struct RopeView {
+  const double* frequencies;   // null: nothing is rotated
+  float amplitude;
+  int32_t half;                // pairs
+  int32_t interleaved;
+};
+
+struct RotateArgs {
+  RopeView rope;
+  const void* x;
+  void* out;
+  int64_t x_stride, out_stride;
+  const int32_t* positions;
+  int32_t tokens, heads, head_dim, dtype;
+};
+
+struct AppendArgs {
+  KvView kv;
+  RopeView rope;
+  const int32_t* starts;       // null: max_new rows each
+  int32_t total_rows, max_new;
+  const int32_t* positions;    // null: the number of the token
+  const void* q;               // may be null, with q_out
+  void* q_out;
+  const void* k_new;
+  const void* v_new;
+  int64_t q_stride, k_stride, v_stride;
+  int32_t q_dtype, kv_dtype;
+};
+
+struct PromptArgs {
+  KvView kv;
+  const void* q;
+  const int32_t* starts;       // null: max_new rows each
+  int32_t total_rows, max_new;
+  void* out;
+  float* lse;                  // may be null
+  int32_t q_dtype, kv_dtype;
+  bool generic;                // PILLAR_FLAG_GENERIC_KERNELS: fp32 arithmetic whatever the types
+  void* workspace;
+};
+
+struct LogprobArgs {
+  const void* logits;
+  int32_t dtype, rows, vocab;
+  int64_t row_stride;
+  float scale;
+  const int32_t* tokens;
+  int32_t num_tokens;
+  float* logprobs;
+  float* lse;                  // may be null
+  float* entropy;              // may be null
+  int32_t top;
+  int32_t* top_ids;
+  float* top_logprobs;
+  void* workspace;
+};
+
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
+hipError_t launch_append_rotated(const AppendArgs& a, hipStream_t s);
+bool prompt_counts(const KvView& kv, int total_rows, int max_new);           // the units of work can be counted in 32 bits
+size_t prompt_workspace(const KvView& kv, int total_rows, int max_new);
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t s);
+size_t logprobs_workspace(int rows, int vocab, int top);
+hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
+
 // process-wide tuning knobs (pillar_set_option); 0 = default
 struct Options {
   int verify_waves = 0;   // wavefronts per compute unit of the two verification passes

@@ -3,6 +3,8 @@
 // synchronises (the optional profiler aside).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <map>
 #include <mutex>
@@ -132,6 +134,24 @@ bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
 
 // requests and heads are the second and third dimension of a grid
 bool fits_a_grid(const pillar_kv_t* kv) { return kv->batch <= 65535 && kv->num_kv_heads <= 65535; }
+
+// bytes from the first to past the last element of strided rows
+uint64_t span_of(int64_t rows, int64_t stride, int64_t row, int esz) { return static_cast<uint64_t>((rows - 1) * stride + row) * esz; }
+
+// packed rows of new tokens
+int check_rows(const pillar_kv_t* kv, const int32_t* starts, int total_rows, int max_new) {
+  if (total_rows < 0 || max_new < 1) return PILLAR_EINVAL;
+  if (!starts && static_cast<int64_t>(kv->batch) * max_new != total_rows) return PILLAR_EINVAL;
+  return fits_a_grid(kv) ? PILLAR_OK : PILLAR_EUNSUPPORTED;
+}
+
+int make_rope(const pillar_rope_t* rope, int head_dim, RopeView* v) {
+  if (rope->rotary_dim < 2 || rope->rotary_dim % 2 != 0 || rope->rotary_dim > head_dim || rope->reserved != 0) return PILLAR_EINVAL;
+  if (rope->layout != PILLAR_ROPE_HALVES && rope->layout != PILLAR_ROPE_INTERLEAVED) return PILLAR_EUNSUPPORTED;
+  if (!std::isfinite(rope->amplitude) || !rope->frequencies || reinterpret_cast<uintptr_t>(rope->frequencies) % 8 != 0) return PILLAR_EINVAL;
+  *v = RopeView{rope->frequencies, rope->amplitude, rope->rotary_dim / 2, rope->layout == PILLAR_ROPE_INTERLEAVED ? 1 : 0};
+  return PILLAR_OK;
+}
 
 int check_nodes(const pillar_kv_t* kv, int max_nodes) {
   if (max_nodes < 1) return PILLAR_EINVAL;
@@ -593,6 +613,182 @@ int pillar_evict_kv(const pillar_kv_t* kv, const float* scores, int64_t score_st
   a.kv_dtype = kv->kv_dtype;
   a.workspace = workspace;
   return launch_evict(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+int pillar_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, int32_t original_len, double fast, double slow,
+                            double* frequencies, float* amplitude) {
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || !(base > 0.0) || !std::isfinite(base) || !frequencies || !amplitude) return PILLAR_EINVAL;
+  if (scaling < PILLAR_ROPE_NONE || scaling > PILLAR_ROPE_BANDS) return PILLAR_EUNSUPPORTED;
+  if (scaling != PILLAR_ROPE_NONE && (!(factor > 0.0) || !std::isfinite(factor))) return PILLAR_EINVAL;
+  const bool by_turns = scaling == PILLAR_ROPE_RAMP || scaling == PILLAR_ROPE_BANDS;
+  if (by_turns && (original_len < 1 || !(slow > 0.0) || !(fast > slow) || !std::isfinite(fast))) return PILLAR_EINVAL;
+  if (scaling == PILLAR_ROPE_RAMP && base == 1.0) return PILLAR_EINVAL;        // all pairs turn alike: there is no ramp
+  const double r = rotary_dim, turn = 6.283185307179586476925;
+  const double b = scaling == PILLAR_ROPE_BASE ? base * std::pow(factor, r / std::max(r - 2.0, 1.0)) : base;
+  auto pair_of = [&](double turns) { return r * std::log(original_len / (turn * turns)) / (2.0 * std::log(base)); };
+  double low = 0.0, high = 0.0;
+  if (scaling == PILLAR_ROPE_RAMP) {
+    low = std::max(std::floor(pair_of(fast)), 0.0);
+    high = std::min(std::ceil(pair_of(slow)), r - 1.0);
+  }
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const double f = std::pow(b, -2.0 * i / r);
+    double stays = 1.0;                                  // share of the frequency that is not stretched
+    if (scaling == PILLAR_ROPE_LINEAR) stays = 0.0;
+    else if (scaling == PILLAR_ROPE_RAMP) stays = 1.0 - std::min(std::max((i - low) / std::max(high - low, 0.001), 0.0), 1.0);
+    else if (scaling == PILLAR_ROPE_BANDS) stays = std::min(std::max((original_len * f / turn - slow) / (fast - slow), 0.0), 1.0);
+    frequencies[i] = stays == 1.0 ? f : f * stays + f / factor * (1.0 - stays);
+  }
+  *amplitude = scaling == PILLAR_ROPE_RAMP ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.f;
+  return PILLAR_OK;
+}
+
+int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_heads, int32_t head_dim, int32_t dtype, const int32_t* positions,
+                  const pillar_rope_t* rope, void* out, int64_t out_stride, void* hip_stream) {
+  if (tokens < 0 || num_heads < 1 || head_dim < 2 || head_dim % 2 != 0) return PILLAR_EINVAL;
+  if (dtype != PILLAR_F32 && dtype != PILLAR_BF16) return PILLAR_EUNSUPPORTED;
+  if (head_dim > 512 || num_heads > 65535) return PILLAR_EUNSUPPORTED;
+  if (!rope || (tokens > 0 && (!x || !positions || !out))) return PILLAR_EINVAL;
+  const int64_t row = static_cast<int64_t>(num_heads) * head_dim;
+  if (x_stride < row || out_stride < row) return PILLAR_EINVAL;
+  RotateArgs a;
+  const int rc = make_rope(rope, head_dim, &a.rope);
+  if (rc != PILLAR_OK) return rc;
+  if (tokens == 0) return PILLAR_OK;
+  const int esz = dtype == PILLAR_F32 ? 4 : 2;
+  const bool in_place = x == out && x_stride == out_stride;
+  if (!in_place && overlap(x, span_of(tokens, x_stride, row, esz), out, span_of(tokens, out_stride, row, esz))) return PILLAR_EINVAL;
+  a.x = x;
+  a.out = out;
+  a.x_stride = x_stride;
+  a.out_stride = out_stride;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.heads = num_heads;
+  a.head_dim = head_dim;
+  a.dtype = dtype;
+  return launch_rotate(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, const int32_t* starts, int32_t total_rows, int32_t max_new,
+                          const int32_t* positions, const void* q, int64_t q_stride, void* q_out, const void* k_new, int64_t k_stride,
+                          const void* v_new, int64_t v_stride, void* hip_stream) {
+  int rc = check_kv(kv);
+  if (rc != PILLAR_OK) return rc;
+  rc = check_rows(kv, starts, total_rows, max_new);
+  if (rc != PILLAR_OK) return rc;
+  if (total_rows > 0 && (!k_new || !v_new || !q != !q_out)) return PILLAR_EINVAL;
+  const int64_t q_row = static_cast<int64_t>(kv->num_q_heads) * kv->head_dim, kv_row = static_cast<int64_t>(kv->num_kv_heads) * kv->head_dim;
+  if (k_stride < kv_row || v_stride < kv_row || (q && q_stride < q_row)) return PILLAR_EINVAL;
+  AppendArgs a;
+  a.rope = RopeView{nullptr, 1.f, 0, 0};
+  if (rope) {
+    rc = make_rope(rope, kv->head_dim, &a.rope);
+    if (rc != PILLAR_OK) return rc;
+  }
+  if (total_rows == 0) return PILLAR_OK;
+  const int esz = kv->q_dtype == PILLAR_F32 ? 4 : 2;
+  if (q) {
+    const uint64_t out_span = span_of(total_rows, q_row, q_row, esz);
+    const bool in_place = q == q_out && q_stride == q_row;
+    if ((!in_place && overlap(q, span_of(total_rows, q_stride, q_row, esz), q_out, out_span)) ||
+        overlap(k_new, span_of(total_rows, k_stride, kv_row, esz), q_out, out_span) ||
+        overlap(v_new, span_of(total_rows, v_stride, kv_row, esz), q_out, out_span))
+      return PILLAR_EINVAL;
+  }
+  a.kv = make_view(kv);
+  const auto bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) | reinterpret_cast<uintptr_t>(k_new) |
+                    reinterpret_cast<uintptr_t>(v_new) | static_cast<uintptr_t>(k_stride * esz) | static_cast<uintptr_t>(v_stride * esz) |
+                    (q ? static_cast<uintptr_t>(q_stride * esz) : 0);
+  if ((bits & 15u) != 0 || !rows_aligned(a.kv, kv->kv_dtype)) return PILLAR_EUNSUPPORTED;
+  a.starts = starts;
+  a.total_rows = total_rows;
+  a.max_new = max_new;
+  a.positions = positions;
+  a.q = q;
+  a.q_out = q_out;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_dtype = kv->q_dtype;
+  a.kv_dtype = kv->kv_dtype;
+  return launch_append_rotated(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+size_t pillar_prompt_workspace_bytes(const pillar_kv_t* kv, int32_t total_rows, int32_t max_new) {
+  if (check_kv(kv) != PILLAR_OK || total_rows < 0 || max_new < 1 || !fits_a_grid(kv)) return 0;
+  const KvView v = make_view(kv);
+  return prompt_counts(v, total_rows, max_new) ? prompt_workspace(v, total_rows, max_new) : 0;
+}
+
+int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* starts, int32_t total_rows, int32_t max_new, void* out, float* lse,
+                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_kv(kv);
+  if (rc != PILLAR_OK) return rc;
+  rc = check_rows(kv, starts, total_rows, max_new);
+  if (rc != PILLAR_OK) return rc;
+  if (total_rows > 0 && (!q || !out)) return PILLAR_EINVAL;
+  PromptArgs a;
+  a.kv = make_view(kv);
+  if (!prompt_counts(a.kv, total_rows, max_new)) return PILLAR_EUNSUPPORTED;
+  rc = check_workspace(workspace, workspace_bytes, prompt_workspace(a.kv, total_rows, max_new));
+  if (rc != PILLAR_OK) return rc;
+  if (total_rows == 0) return PILLAR_OK;
+  // several workgroups read a row of q, and one of them writes its result
+  const uint64_t bytes = static_cast<uint64_t>(total_rows) * kv->num_q_heads * kv->head_dim * (kv->q_dtype == PILLAR_F32 ? 4 : 2);
+  if (overlap(q, bytes, out, bytes)) return PILLAR_EINVAL;
+  a.q = q;
+  a.starts = starts;
+  a.total_rows = total_rows;
+  a.max_new = max_new;
+  a.out = out;
+  a.lse = lse;
+  a.q_dtype = kv->q_dtype;
+  a.kv_dtype = kv->kv_dtype;
+  a.generic = (kv->flags & PILLAR_FLAG_GENERIC_KERNELS) != 0;
+  a.workspace = workspace;
+  return launch_prompt(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
+}
+
+size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
+  if (rows < 0 || vocab < 1 || top < 0 || top > kMostAlternatives) return 0;
+  return std::max<size_t>(256, logprobs_workspace(rows, vocab, top));
+}
+
+int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, float scale, const int32_t* tokens,
+                          int32_t num_tokens, float* logprobs, float* lse, float* entropy, int32_t top, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (rows < 0 || vocab < 1 || row_stride < vocab || num_tokens < 0 || top < 0) return PILLAR_EINVAL;
+  if (!(scale > 0.f) || !(scale < 1e30f)) return PILLAR_EINVAL;
+  if (dtype != PILLAR_F32 && dtype != PILLAR_BF16) return PILLAR_EUNSUPPORTED;
+  if (top > kMostAlternatives) return PILLAR_EUNSUPPORTED;
+  if (rows == 0) return PILLAR_OK;
+  if (!logits) return PILLAR_EINVAL;
+  if ((num_tokens > 0) != (tokens != nullptr) || (num_tokens > 0) != (logprobs != nullptr)) return PILLAR_EINVAL;
+  if ((top > 0) != (top_ids != nullptr) || (top > 0) != (top_logprobs != nullptr)) return PILLAR_EINVAL;
+  const uintptr_t esz = dtype == PILLAR_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % esz != 0) return PILLAR_EUNSUPPORTED;
+  const int rc = check_workspace(workspace, workspace_bytes, pillar_logprobs_workspace_bytes(rows, vocab, top));
+  if (rc != PILLAR_OK) return rc;
+  LogprobArgs a;
+  a.logits = logits;
+  a.dtype = dtype;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.row_stride = row_stride;
+  a.scale = scale;
+  a.tokens = tokens;
+  a.num_tokens = num_tokens;
+  a.logprobs = logprobs;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.top = top;
+  a.top_ids = top_ids;
+  a.top_logprobs = top_logprobs;
+  a.workspace = workspace;
+  return launch_logprobs(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
 }
 
 int pillar_set_option(const char* name, int64_t value) {
