@@ -8,8 +8,9 @@
 //   logprob_pass   a workgroup per (row, part of the row): (M, S, A) and the `top` largest of the part
 //   logprob_join   a workgroup per row: joins the parts, looks the given tokens up
 //
-// The largest logits are kept by each wavefront as one sorted list over its 64 lanes.  A logit gets in when it is larger than the list's last, which after
-// a few hundred logits is rare; the maximum of a lane's batch of logits, needed for the reference anyway, says whether to look.
+// The largest logits are kept by each wavefront as one sorted list over its 64 lanes.  A logit gets in when it comes before the list's last, which after
+// a few batches is rare; the maximum of a lane's batch, needed for m anyway, says whether to look.  Where many lanes have something (the first
+// batch, a row that rises), the `top`-th of the lanes' maxima is a bound that as many logits reach, so little more than `top` are tried.
 #include <algorithm>
 
 #include "launch.hpp"
@@ -24,7 +25,7 @@ constexpr int kNoId = INT32_MAX;
 struct Params {
   LogprobArgs a;
   float c;                     // scale * log2 e
-  int32_t parts, each;         // parts of a row, logits of a part (a multiple of 16)
+  int32_t parts, each;         // parts of a row, vectors of 16 bytes of a part
   float* msa;                  // [rows][parts][4]
   float2* lists;               // [rows][parts][top]: logit, id (as bits)
 };
@@ -87,52 +88,232 @@ struct List {
 template <int DT>
 __device__ __forceinline__ float logit(const void* p, int64_t i) { return Storage<DT>::load(p, i); }
 
-// TOP: a list is wanted
+constexpr int kLoads = 4;                                // 16-byte loads of a lane in a batch
+
+// One wavefront's share of a row.
+template <int DT, bool TOP>
+struct Scan {
+  static constexpr int V = DT == PILLAR_F32 ? 4 : 8, kBatch = kLoads * V;
+  Sums sums;
+  List list;
+  float least;                 // the list's last of `top`
+  int least_id;
+  float c;
+  int top, lane;
+
+  __device__ __forceinline__ Scan(float c_, int top_) : sums{-INFINITY, 0.f, 0.f}, least(-INFINITY), least_id(kNoId), c(c_), top(top_), lane(threadIdx.x & 63) { list.clear(); }
+
+  __device__ __forceinline__ void offer(float x, int id, float bound) {
+    for (uint64_t some = __ballot(x >= bound && before(x, id, least, least_id)); some;) {
+      const int from = __builtin_ctzll(some);
+      list.insert(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), from)), __builtin_amdgcn_readlane(id, from));
+      least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.x), top - 1));
+      least_id = __builtin_amdgcn_readlane(list.id, top - 1);
+      some &= some - 1;
+      some &= __ballot(before(x, id, least, least_id));
+    }
+  }
+
+  // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th
+  template <int N, typename Id>
+  __device__ __forceinline__ void take(const float (&x)[N], Id id) {
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+    // the reference moves only for a logit that exceeds it by more than 8 (log2): 2^y stays below 2^8
+    const bool moves = (most - sums.m) * c > 8.f || (sums.m == -INFINITY && most > -INFINITY);
+    if (__any(moves)) {
+      if (moves) sums.move(most, c);
+    }
+    const float m = sums.m == -INFINITY ? 0.f : sums.m;
+    float s[2] = {0.f, 0.f}, a[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = (x[i] - m) * c, e = __builtin_amdgcn_exp2f(y);
+      s[i & 1] += e;
+      a[i & 1] = __builtin_fmaf(e, fmaxf(y, -200.f), a[i & 1]);          // (-inf: 0 * -200)
+    }
+    sums.s += s[0] + s[1];
+    sums.a += a[0] + a[1];
+    if constexpr (TOP) {
+      const uint64_t some = __ballot(most > least);
+      if (some) {
+        float bound = least;
+        if (__builtin_popcountll(some) > top) bound = nth_of_lanes(most);
+#pragma unroll
+        for (int i = 0; i < N; ++i) offer(x[i], id(i), bound);
+      }
+    }
+  }
+
+  // the `top`-th largest of the lanes' values
+  __device__ __forceinline__ float nth_of_lanes(float x) const {
+#pragma unroll
+    for (int k = 2; k <= 64; k <<= 1)
+#pragma unroll
+      for (int o = k >> 1; o > 0; o >>= 1) {
+        const float other = __shfl_xor(x, o);
+        x = ((lane & o) == 0) == ((lane & k) == 0) ? fmaxf(x, other) : fminf(x, other);
+      }
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), top - 1));
+  }
+
+  static __device__ __forceinline__ void unpack(const u32x4 (&raw)[kLoads], float (&x)[kBatch]) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        x[u * V + j] = DT == PILLAR_F32 ? __uint_as_float(raw[u][j & 3]) : __uint_as_float((j & 1) ? raw[u][(j >> 1) & 3] & 0xffff0000u : raw[u][(j >> 1) & 3] << 16);
+  }
+
+  // vectors v0 .. v1 - 1 of 16 bytes, kWaves wavefronts in turn; the first logit of vector 0 is number `first`
+  __device__ __forceinline__ void vectors(const u32x4* p, int v0, int v1, int first, int wave) {
+    constexpr int kStep = 64 * kLoads;
+    if (v0 >= v1) return;
+    u32x4 raw[kLoads];
+    auto fetch = [&](int v) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) raw[u] = p[min(v + 64 * u + lane, v1 - 1)];
+    };
+    int v = v0 + wave * kStep;
+    if (v >= v1) return;
+    fetch(v);
+    for (; v < v1; v += kWaves * kStep) {
+      float x[kBatch];
+      unpack(raw, x);
+      const int at = v;
+      if (v + kWaves * kStep < v1) fetch(v + kWaves * kStep);
+      if (at + kStep > v1) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = at + 64 * (i / V) + lane < v1 ? x[i] : -INFINITY;
+      }
+      take(x, [&](int i) { return first + (at + 64 * (i / V) + lane) * V + i % V; });
+    }
+  }
+};
+
+// What a row says, once its sums are known.
+template <int DT>
+struct Row {
+  const LogprobArgs& a;
+  int r;
+  int64_t at;                  // its first element
+  Sums sums;
+  float log_s;                 // in natural units
+  bool nan, empty, endless;
+
+  __device__ __forceinline__ Row(const LogprobArgs& a_, int r_) : a(a_), r(r_), at(r_ * a_.row_stride) {}
+  // (all threads of a workgroup) m = -inf: nothing but -inf (and NaN); +inf: the sum is NaN, from inf - inf, and whether the row has NaN too has to be looked up
+  __device__ __forceinline__ void settle(Sums s) {
+    sums = s;
+    log_s = kLn2 * log2f(s.s);
+    endless = s.m == INFINITY, empty = s.m == -INFINITY;
+    nan = s.s != s.s;
+    if (endless) {
+      bool mine = false;
+      for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
+        const float x = logit<DT>(a.logits, at + i);
+        mine |= x != x;
+      }
+      nan = __syncthreads_or(mine);
+    }
+  }
+  __device__ __forceinline__ float log_prob(float x) const {
+    if (nan) return NAN;
+    if (empty) return -INFINITY;
+    if (endless) return x < INFINITY ? -INFINITY : NAN;
+    return __builtin_fmaf(x - sums.m, a.scale, -log_s);
+  }
+  // the j-th given token: its logit, or NaN where there is no such token
+  __device__ __forceinline__ bool given(int j, float& x) const {
+    const int id = a.tokens[static_cast<int64_t>(r) * a.num_tokens + j];
+    const bool there = id >= 0 && id < a.vocab;
+    x = there ? logit<DT>(a.logits, at + id) : 0.f;
+    return there;
+  }
+  __device__ __forceinline__ void put(int j, bool there, float x) const {
+    a.logprobs[static_cast<int64_t>(r) * a.num_tokens + j] = there ? log_prob(x) : -INFINITY;
+  }
+  __device__ __forceinline__ void put_sums() const {
+    if (a.lse) a.lse[r] = nan ? NAN : empty ? -INFINITY : endless ? INFINITY : __builtin_fmaf(a.scale, sums.m, log_s);
+    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty ? 0.f : log_s - kLn2 * (sums.a / sums.s);
+  }
+  // (one wavefront) Fewer numbers above -inf than wanted: the first of -inf, then the first that are none at all.
+  __device__ __forceinline__ void put_list(List list) const {
+    const int lane = threadIdx.x & 63;
+    int have = __builtin_popcountll(__ballot(list.x > -INFINITY));
+    for (int none = 0; none < 2 && have < a.top; ++none)
+      for (int i0 = 0; i0 < a.vocab && have < a.top; i0 += 64) {
+        const float x = i0 + lane < a.vocab ? logit<DT>(a.logits, at + i0 + lane) : 0.f;
+        for (uint64_t some = __ballot(none ? x != x : x == -INFINITY); some && have < a.top; some &= some - 1, ++have) {
+          if (lane == have) { list.x = none ? NAN : -INFINITY; list.id = i0 + __builtin_ctzll(some); }
+        }
+      }
+    if (lane < a.top) {
+      const int64_t to = static_cast<int64_t>(r) * a.top + lane;
+      a.top_ids[to] = lane < have ? list.id : -1;
+      a.top_logprobs[to] = lane < have ? log_prob(list.x) : -INFINITY;
+    }
+  }
+};
+
+__device__ __forceinline__ Sums over_lanes(Sums s, float c) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s.add(Sums{__shfl_xor(s.m, o), __shfl_xor(s.s, o), __shfl_xor(s.a, o)}, c);
+  return s;
+}
+
+// TOP: a list is wanted.  Rows of one part are done here.
 template <int DT, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
-  constexpr int V = DT == PILLAR_F32 ? 4 : 8;
+  using S = Scan<DT, TOP>;
+  constexpr int V = S::V, kSize = DT == PILLAR_F32 ? 4 : 2;
   __shared__ Sums s_sums[kWaves];
   __shared__ float s_x[kWaves][64];
   __shared__ int s_id[kWaves][64];
   const LogprobArgs& a = p.a;
   const int r = blockIdx.x / p.parts, part = blockIdx.x - r * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = r * a.row_stride;
-  const int begin = part * p.each, end = min(a.vocab, begin + p.each);
-  Sums sums{-INFINITY, 0.f, 0.f};
-  List list;
-  list.clear();
-  float least = -INFINITY;                               // the list's last of `top`
-  for (int i0 = begin + wave * 64; i0 < end; i0 += kThreads) {
-    const int i = i0 + lane;
-    const float x = i < end ? logit<DT>(a.logits, row + i) : -INFINITY;
-    if (x > sums.m) sums.move(x, p.c);
-    const float y = (x - (sums.m == -INFINITY ? 0.f : sums.m)) * p.c;
-    const float e = __builtin_amdgcn_exp2f(y);
-    sums.s += e;
-    sums.a = __builtin_fmaf(e, fmaxf(y, -200.f), sums.a);
-    if (TOP) {
-      for (uint64_t over = __ballot(x > least); over; over &= over - 1) {
-        const int from = __builtin_ctzll(over);
-        list.insert(__shfl(x, from), i0 + from);
-      }
-      least = __shfl(list.x, a.top - 1);
-    }
+  Row<DT> row(a, r);
+  float given = 0.f;
+  bool is_given = false;
+  if (p.parts == 1 && tid < a.num_tokens) is_given = row.given(tid, given);                  // (on its way beside the row)
+  // the row up to the first multiple of 16 bytes, vectors of 16 bytes, the rest
+  const char* const base = static_cast<const char*>(a.logits) + row.at * kSize;
+  const int head = min(a.vocab, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(base) & 15u)) & 15u) / kSize);
+  const int whole = (a.vocab - head) / V, rest = a.vocab - head - whole * V;
+  S scan(p.c, a.top);
+  scan.vectors(reinterpret_cast<const u32x4*>(base + head * kSize), part * p.each, min(whole, (part + 1) * p.each), head, wave);
+  if (part == 0 && wave == kWaves - 1) {                 // what is left of the row at both ends, less than 16 logits
+    const int id = lane < head ? lane : a.vocab - rest + lane - head;
+    const float x[1] = {lane < head + rest ? logit<DT>(a.logits, row.at + id) : -INFINITY};
+    scan.take(x, [&](int) { return id; });
   }
-  (void)V;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sums.add(Sums{__shfl_xor(sums.m, o), __shfl_xor(sums.s, o), __shfl_xor(sums.a, o)}, p.c);
+  const Sums sums = over_lanes(scan.sums, p.c);
   if (lane == 0) s_sums[wave] = sums;
-  if (TOP) { s_x[wave][lane] = list.x; s_id[wave][lane] = list.id; }
+  if (TOP) { s_x[wave][lane] = scan.list.x; s_id[wave][lane] = scan.list.id; }
   __syncthreads();
-  if (wave > 0) return;
-  const int64_t slot = static_cast<int64_t>(r) * p.parts + part;
+  Sums all = s_sums[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    sums.add(s_sums[w], p.c);
-    if (TOP) list.merge(s_x[w][lane], s_id[w][lane]);
+  for (int w = 1; w < kWaves; ++w) all.add(s_sums[w], p.c);
+  List list = scan.list;
+  if (TOP && wave == 0) {
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) list.merge(s_x[w][lane], s_id[w][lane]);
   }
-  if (lane == 0) *reinterpret_cast<f32x4_t*>(p.msa + 4 * slot) = f32x4_t{sums.m, sums.s, sums.a, 0.f};
-  if (TOP && lane < a.top) p.lists[slot * a.top + lane] = make_float2(list.x, __int_as_float(list.id));
+  if (p.parts > 1) {
+    const int64_t slot = static_cast<int64_t>(r) * p.parts + part;
+    if (tid == 0) *reinterpret_cast<f32x4_t*>(p.msa + 4 * slot) = f32x4_t{all.m, all.s, all.a, 0.f};
+    if (TOP && wave == 0 && lane < a.top) p.lists[slot * a.top + lane] = make_float2(list.x, __int_as_float(list.id));
+    return;
+  }
+  row.settle(all);
+  if (tid == 0) row.put_sums();
+  if (tid < a.num_tokens) row.put(tid, is_given, given);
+  for (int j = tid + kThreads; j < a.num_tokens; j += kThreads) {
+    is_given = row.given(j, given);
+    row.put(j, is_given, given);
+  }
+  if (TOP && wave == 0) row.put_list(list);
 }
 
 template <int DT, bool TOP>
@@ -142,14 +323,17 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
   __shared__ int s_id[kWaves][64];
   const LogprobArgs& a = p.a;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = r * a.row_stride, slot = static_cast<int64_t>(r) * p.parts;
+  const int64_t slot = static_cast<int64_t>(r) * p.parts;
+  Row<DT> row(a, r);
+  float given = 0.f;
+  bool is_given = false;
+  if (tid < a.num_tokens) is_given = row.given(tid, given);
   Sums sums{-INFINITY, 0.f, 0.f};
   for (int i = tid; i < p.parts; i += kThreads) {
     const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p.msa + 4 * (slot + i));
     sums.add(Sums{v[0], v[1], v[2]}, p.c);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sums.add(Sums{__shfl_xor(sums.m, o), __shfl_xor(sums.s, o), __shfl_xor(sums.a, o)}, p.c);
+  sums = over_lanes(sums, p.c);
   if (lane == 0) s_sums[wave] = sums;
   List list;
   list.clear();
@@ -166,62 +350,31 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
   sums = s_sums[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sums.add(s_sums[w], p.c);
-  // m = -inf: nothing but -inf (and NaN); +inf: the sum is NaN, from inf - inf, and whether the row has NaN too has to be looked up
-  const float log_s = log2f(sums.s);
-  const bool endless = sums.m == INFINITY, empty = sums.m == -INFINITY;
-  bool nan = sums.s != sums.s;
-  if (endless) {
-    bool mine = false;
-    for (int i = tid; i < a.vocab; i += kThreads) {
-      const float x = logit<DT>(a.logits, row + i);
-      mine |= x != x;
-    }
-    nan = __syncthreads_or(mine);
-  }
-  auto log_prob = [&](float x) {
-    if (nan) return NAN;
-    if (empty) return -INFINITY;
-    if (endless) return x < INFINITY ? -INFINITY : NAN;
-    return __builtin_fmaf(x - sums.m, a.scale, -kLn2 * log_s);
-  };
-  if (tid == 0) {
-    if (a.lse) a.lse[r] = nan ? NAN : empty ? -INFINITY : endless ? INFINITY : __builtin_fmaf(a.scale, sums.m, kLn2 * log_s);
-    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty ? 0.f : kLn2 * (log_s - sums.a / sums.s);
-  }
-  for (int j = tid; j < a.num_tokens; j += kThreads) {
-    const int id = a.tokens[static_cast<int64_t>(r) * a.num_tokens + j];
-    a.logprobs[static_cast<int64_t>(r) * a.num_tokens + j] = id >= 0 && id < a.vocab ? log_prob(logit<DT>(a.logits, row + id)) : -INFINITY;
+  row.settle(sums);
+  if (tid == 0) row.put_sums();
+  if (tid < a.num_tokens) row.put(tid, is_given, given);
+  for (int j = tid + kThreads; j < a.num_tokens; j += kThreads) {
+    is_given = row.given(j, given);
+    row.put(j, is_given, given);
   }
   if (!TOP || wave > 0) return;
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) list.merge(s_x[w][lane], s_id[w][lane]);
-  // Fewer numbers above -inf than wanted: the first of -inf, then the first that are none at all.
-  int have = __builtin_popcountll(__ballot(list.x > -INFINITY));
-  for (int nan = 0; nan < 2 && have < a.top; ++nan)
-    for (int i0 = 0; i0 < a.vocab && have < a.top; i0 += 64) {
-      const float x = i0 + lane < a.vocab ? logit<DT>(a.logits, row + i0 + lane) : 0.f;
-      for (uint64_t some = __ballot(nan ? x != x : x == -INFINITY); some && have < a.top; some &= some - 1, ++have) {
-        const int from = __builtin_ctzll(some);
-        if (lane == have) { list.x = nan ? NAN : -INFINITY; list.id = i0 + from; }
-      }
-    }
-  if (lane < a.top) {
-    const int64_t to = static_cast<int64_t>(r) * a.top + lane;
-    a.top_ids[to] = lane < have ? list.id : -1;
-    a.top_logprobs[to] = lane < have ? log_prob(list.x) : -INFINITY;
-  }
+  row.put_list(list);
 }
 
 struct Plan {
   int parts, each;
 };
-Plan plan_of(int rows, int vocab) {
-  const int64_t wanted = (4 * 256 + rows - 1) / std::max(rows, 1);
-  const int most = (vocab + 4095) / 4096;
+// Two workgroups to a compute unit, in parts of 4096 bf16 or 2048 fp32 logits at the least.
+Plan plan_of(int rows, int vocab, int dtype) {
+  const int per = dtype == PILLAR_F32 ? 4 : 8, vectors = vocab / per;
+  const int64_t wanted = (2 * static_cast<int64_t>(num_cus()) + rows - 1) / std::max(rows, 1);
+  const int most = (vectors + 511) / 512;
   Plan p;
   p.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(wanted, most)));
-  p.each = (((vocab + p.parts - 1) / p.parts) + 15) / 16 * 16;
-  p.parts = (vocab + p.each - 1) / p.each;
+  p.each = std::max(1, (vectors + p.parts - 1) / p.parts);
+  p.parts = std::max(1, (vectors + p.each - 1) / p.each);
   return p;
 }
 
@@ -231,6 +384,7 @@ hipError_t launch(const Params& p, hipStream_t s) {
     KernelTimer timer("logprob_pass", s);
     hipLaunchKernelGGL((logprob_pass<DT, TOP>), dim3(static_cast<unsigned>(p.parts) * p.a.rows), dim3(kThreads), 0, s, p);
   }
+  if (p.parts == 1) return hipGetLastError();
   KernelTimer timer("logprob_join", s);
   hipLaunchKernelGGL((logprob_join<DT, TOP>), dim3(p.a.rows), dim3(kThreads), 0, s, p);
   return hipGetLastError();
@@ -238,13 +392,14 @@ hipError_t launch(const Params& p, hipStream_t s) {
 
 }  // namespace
 
+// (whatever the type)
 size_t logprobs_workspace(int rows, int vocab, int top) {
-  const Plan p = plan_of(rows, vocab);
-  return align_up(static_cast<size_t>(rows) * p.parts * 16, 256) + static_cast<size_t>(rows) * p.parts * top * 8;
+  const size_t parts = std::max(plan_of(rows, vocab, PILLAR_F32).parts, plan_of(rows, vocab, PILLAR_BF16).parts);
+  return align_up(rows * parts * 16, 256) + rows * parts * top * 8;
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
-  const Plan plan = plan_of(a.rows, a.vocab);
+  const Plan plan = plan_of(a.rows, a.vocab, a.dtype);
   Params p;
   p.a = a;
   p.c = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
