@@ -9,10 +9,16 @@
 //   logprob_join   a workgroup per row: joins the parts, looks the given tokens up
 //
 // The largest logits are kept by each wavefront as one sorted list over its 64 lanes.  A logit gets in when it comes before the list's last, which after
-// a few batches is rare; the maximum of a lane's batch, needed for m anyway, says whether to look.  Where many lanes have something (the first
-// batch, a row that rises), the `top`-th of the lanes' maxima is a bound that as many logits reach, so little more than `top` are tried.
+// a few batches is rare; the maximum of a lane's batch, needed for m anyway, says whether to look.
+//
+// What bounds it: the rows at 4.4 TB/s (640 rows of 150000 bf16 logits: 44 us without alternatives; the same without the exponentials 39), and what the lists
+// cost, 5 us with one alternative, 15 with eight.  Branches by what a wavefront is have to be scalar ones (readfirstlane): as lanes of a mask, the loop waited for
+// every load before its next turn.  A key is one whole number, because comparisons of two parts became branches, at every step of a sort.
+// More wavefronts to a row, or more parts, make more lists to fill (512 threads 52 us with one alternative, 256 49; 240 rows of 50001 fp32 with twenty 32 and
+// 28), deeper prefetch gains nothing (three batches 48.4, four 48.7).
 #include <algorithm>
 
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "rope.hpp"
 
@@ -20,15 +26,6 @@ namespace pillar {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kNoId = INT32_MAX;
-
-struct Params {
-  LogprobArgs a;
-  float c;                     // scale * log2 e
-  int32_t parts, each;         // parts of a row, vectors of 16 bytes of a part
-  float* msa;                  // [rows][parts][4]
-  float2* lists;               // [rows][parts][top]: logit, id (as bits)
-};
 
 struct Sums {
   float m, s, a;               // m = -inf: nothing but -inf so far
@@ -50,45 +47,67 @@ struct Sums {
   }
 };
 
-// larger logit, or the same one earlier
-__device__ __forceinline__ bool before(float x, int i, float y, int j) { return x > y || (x == y && i < j); }
+// A logit and its number as one whole number that grows with the logit and, among equal ones (zeros of either sign are equal), towards the lower number.  0: none.
+typedef uint64_t Key;
+__device__ __forceinline__ Key key_of(float x, int id) {
+  const uint32_t u = __float_as_uint(x + 0.f), o = u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+  return static_cast<Key>(o) << 32 | ~static_cast<uint32_t>(id);
+}
+__device__ __forceinline__ float logit_of(Key k) {
+  const uint32_t o = static_cast<uint32_t>(k >> 32);
+  return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ int id_of(Key k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
+__device__ __forceinline__ Key of_lane(Key k, int lane) {
+  return static_cast<Key>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(k >> 32), lane))) << 32 |
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(k), lane));
+}
+
+struct Params {
+  LogprobArgs a;
+  float c;                     // scale * log2 e
+  int32_t parts, each;         // parts of a row, vectors of 16 bytes of a part
+  float* msa;                  // [rows][parts][4]
+  Key* lists;                  // [rows][parts][top]
+};
 
 // A sorted list over the lanes of a wavefront: lane 0 has the largest.
 struct List {
-  float x;
-  int id;
-  __device__ __forceinline__ void clear() { x = -INFINITY; id = kNoId; }
-  __device__ __forceinline__ void insert(float nx, int nid) {            // (the same in all lanes)
-    const bool mine = before(x, id, nx, nid);
-    const int at = __builtin_popcountll(__ballot(mine));
-    const int lane = threadIdx.x & 63;
-    const float ux = __shfl_up(x, 1);
-    const int uid = __shfl_up(id, 1);
-    if (!mine) {
-      x = lane == at ? nx : ux;
-      id = lane == at ? nid : uid;
-    }
+  Key key = 0;
+  __device__ __forceinline__ void insert(Key k) {        // (the same in all lanes)
+    const bool before = key > k;
+    const int at = __builtin_popcountll(__ballot(before)), lane = threadIdx.x & 63;
+    const Key up = lane_before(key), other = lane == at ? k : up;
+    key = before ? key : other;
   }
   // the best 64 of both, sorted
-  __device__ __forceinline__ void merge(float ox, int oid) {
-    const int lane = threadIdx.x & 63;
-    const float rx = __shfl(ox, 63 - lane);
-    const int rid = __shfl(oid, 63 - lane);
-    if (before(rx, rid, x, id)) { x = rx; id = rid; }    // a sequence that rises and falls, of the best 64
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float px = __shfl_xor(x, o);
-      const int pid = __shfl_xor(id, o);
-      const bool take = (lane & o) ? before(x, id, px, pid) : before(px, pid, x, id);
-      if (take) { x = px; id = pid; }
-    }
+  __device__ __forceinline__ void merge(Key o) {
+    const Key r = lane_reversed(o);
+    key = key > r ? key : r;                             // a sequence that rises and falls, of the best 64
+    steps<64, 32>();
+  }
+  template <int K = 2>
+  __device__ __forceinline__ void sort() {
+    steps<K, K / 2>();
+    if constexpr (K < 64) sort<2 * K>();
+  }
+
+ private:
+  // stretches of K lanes that rise and fall, or fall and rise, into order, every second one backwards
+  template <int K, int O>
+  __device__ __forceinline__ void steps() {
+    const Key other = lane_xor<O>(key);
+    const bool larger = ((threadIdx.x & O) == 0) == (K == 64 || (threadIdx.x & K) == 0);
+    key = (key > other) == larger ? key : other;
+    if constexpr (O > 1) steps<K, O / 2>();
   }
 };
 
 template <int DT>
 __device__ __forceinline__ float logit(const void* p, int64_t i) { return Storage<DT>::load(p, i); }
 
-constexpr int kLoads = 4;                                // 16-byte loads of a lane in a batch
+constexpr int kLoads = 2, kAhead = 2;                    // 16-byte loads of a lane in a batch, batches on their way
+constexpr int kFew = 8;                                  // what is put into a list one by one rather than sorted
 
 // One wavefront's share of a row.
 template <int DT, bool TOP>
@@ -97,26 +116,50 @@ struct Scan {
   Sums sums;
   List list;
   float least;                 // the list's last of `top`
-  int least_id;
+  Key least_key;
   float c;
   int top, lane;
 
-  __device__ __forceinline__ Scan(float c_, int top_) : sums{-INFINITY, 0.f, 0.f}, least(-INFINITY), least_id(kNoId), c(c_), top(top_), lane(threadIdx.x & 63) { list.clear(); }
+  __device__ __forceinline__ Scan(float c_, int top_) : sums{-INFINITY, 0.f, 0.f}, least(-INFINITY), least_key(0), c(c_), top(top_), lane(threadIdx.x & 63) {}
 
-  __device__ __forceinline__ void offer(float x, int id, float bound) {
-    for (uint64_t some = __ballot(x >= bound && before(x, id, least, least_id)); some;) {
-      const int from = __builtin_ctzll(some);
-      list.insert(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), from)), __builtin_amdgcn_readlane(id, from));
-      least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.x), top - 1));
-      least_id = __builtin_amdgcn_readlane(list.id, top - 1);
-      some &= some - 1;
-      some &= __ballot(before(x, id, least, least_id));
-    }
+  // What of N logits of every lane gets into the list.  Each lane brings its best (`most`), then its next best as long as some get in: one by one where
+  // they are few, else sorted and merged at once.
+  template <int N, typename Id>
+  __device__ __forceinline__ void enter(float (&x)[N], Id id, float most) {
+    do {
+      int at = 0;
+#pragma unroll
+      for (int i = N - 1; i > 0; --i) at = x[i] == most ? i : at;
+      if (x[0] == most) at = 0;
+      const Key mine = most >= least && most > -INFINITY ? key_of(most, id(at)) : 0;
+      uint64_t some = __ballot(mine > least_key);
+      if (__builtin_popcountll(some) > kFew) {
+        List sorted;
+        sorted.key = mine;
+        sorted.sort();
+        list.merge(sorted.key);
+        least_key = of_lane(list.key, top - 1);
+      } else {
+        while (some) {
+          const int from = __builtin_ctzll(some);
+          list.insert(of_lane(mine, from));
+          least_key = of_lane(list.key, top - 1);
+          some &= some - 1;
+          some &= __ballot(mine > least_key);
+        }
+      }
+      least = least_key ? logit_of(least_key) : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = i == at ? -INFINITY : x[i];
+      most = x[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+    } while (__any(most > least));
   }
 
   // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th
   template <int N, typename Id>
-  __device__ __forceinline__ void take(const float (&x)[N], Id id) {
+  __device__ __forceinline__ void take(float (&x)[N], Id id) {
     float most = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
@@ -136,26 +179,8 @@ struct Scan {
     sums.s += s[0] + s[1];
     sums.a += a[0] + a[1];
     if constexpr (TOP) {
-      const uint64_t some = __ballot(most > least);
-      if (some) {
-        float bound = least;
-        if (__builtin_popcountll(some) > top) bound = nth_of_lanes(most);
-#pragma unroll
-        for (int i = 0; i < N; ++i) offer(x[i], id(i), bound);
-      }
+      if (__any(most > least)) enter(x, id, most);
     }
-  }
-
-  // the `top`-th largest of the lanes' values
-  __device__ __forceinline__ float nth_of_lanes(float x) const {
-#pragma unroll
-    for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-      for (int o = k >> 1; o > 0; o >>= 1) {
-        const float other = __shfl_xor(x, o);
-        x = ((lane & o) == 0) == ((lane & k) == 0) ? fmaxf(x, other) : fminf(x, other);
-      }
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), top - 1));
   }
 
   static __device__ __forceinline__ void unpack(const u32x4 (&raw)[kLoads], float (&x)[kBatch]) {
@@ -166,28 +191,32 @@ struct Scan {
         x[u * V + j] = DT == PILLAR_F32 ? __uint_as_float(raw[u][j & 3]) : __uint_as_float((j & 1) ? raw[u][(j >> 1) & 3] & 0xffff0000u : raw[u][(j >> 1) & 3] << 16);
   }
 
-  // vectors v0 .. v1 - 1 of 16 bytes, kWaves wavefronts in turn; the first logit of vector 0 is number `first`
+  // vectors v0 .. v1 - 1 of 16 bytes, kWaves wavefronts in turn; the first logit of vector 0 is number `first`.  kAhead batches are on their way.
   __device__ __forceinline__ void vectors(const u32x4* p, int v0, int v1, int first, int wave) {
-    constexpr int kStep = 64 * kLoads;
-    if (v0 >= v1) return;
-    u32x4 raw[kLoads];
-    auto fetch = [&](int v) {
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) raw[u] = p[min(v + 64 * u + lane, v1 - 1)];
-    };
+    constexpr int kStep = 64 * kLoads, kNext = kWaves * kStep;
     int v = v0 + wave * kStep;
     if (v >= v1) return;
-    fetch(v);
-    for (; v < v1; v += kWaves * kStep) {
-      float x[kBatch];
-      unpack(raw, x);
-      const int at = v;
-      if (v + kWaves * kStep < v1) fetch(v + kWaves * kStep);
-      if (at + kStep > v1) {
+    u32x4 raw[kAhead][kLoads];
+    auto fetch = [&](u32x4 (&to)[kLoads], int from) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) x[i] = at + 64 * (i / V) + lane < v1 ? x[i] : -INFINITY;
+      for (int u = 0; u < kLoads; ++u) to[u] = __builtin_nontemporal_load(p + min(from + 64 * u + lane, v1 - 1));
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) fetch(raw[k], v + k * kNext);
+    while (true) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        float x[kBatch];
+        unpack(raw[k], x);
+        if (v + kAhead * kNext < v1) fetch(raw[k], v + kAhead * kNext);
+        if (v + kStep > v1) {
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) x[i] = v + 64 * (i / V) + lane < v1 ? x[i] : -INFINITY;
+        }
+        take(x, [&](int i) { return first + (v + 64 * (i / V) + lane) * V + i % V; });          // (V is a power of two)
+        v += kNext;
+        if (v >= v1) return;
       }
-      take(x, [&](int i) { return first + (at + 64 * (i / V) + lane) * V + i % V; });
     }
   }
 };
@@ -241,26 +270,41 @@ struct Row {
   // (one wavefront) Fewer numbers above -inf than wanted: the first of -inf, then the first that are none at all.
   __device__ __forceinline__ void put_list(List list) const {
     const int lane = threadIdx.x & 63;
-    int have = __builtin_popcountll(__ballot(list.x > -INFINITY));
+    float x = logit_of(list.key);
+    int id = id_of(list.key), have = __builtin_popcountll(__ballot(list.key != 0));
     for (int none = 0; none < 2 && have < a.top; ++none)
       for (int i0 = 0; i0 < a.vocab && have < a.top; i0 += 64) {
-        const float x = i0 + lane < a.vocab ? logit<DT>(a.logits, at + i0 + lane) : 0.f;
-        for (uint64_t some = __ballot(none ? x != x : x == -INFINITY); some && have < a.top; some &= some - 1, ++have) {
-          if (lane == have) { list.x = none ? NAN : -INFINITY; list.id = i0 + __builtin_ctzll(some); }
+        const float y = i0 + lane < a.vocab ? logit<DT>(a.logits, at + i0 + lane) : 0.f;
+        for (uint64_t some = __ballot(none ? y != y : y == -INFINITY); some && have < a.top; some &= some - 1, ++have) {
+          if (lane == have) { x = none ? NAN : -INFINITY; id = i0 + __builtin_ctzll(some); }
         }
       }
     if (lane < a.top) {
       const int64_t to = static_cast<int64_t>(r) * a.top + lane;
-      a.top_ids[to] = lane < have ? list.id : -1;
-      a.top_logprobs[to] = lane < have ? log_prob(list.x) : -INFINITY;
+      a.top_ids[to] = lane < have ? id : -1;
+      a.top_logprobs[to] = lane < have ? log_prob(x) : -INFINITY;
     }
   }
 };
 
-__device__ __forceinline__ Sums over_lanes(Sums s, float c) {
+// The lists of a workgroup's wavefronts into the first one's.
+__device__ __forceinline__ void merge_lists(List& list, Key (&s_key)[kWaves][64], int wave, int lane) {
+  s_key[wave][lane] = list.key;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s.add(Sums{__shfl_xor(s.m, o), __shfl_xor(s.s, o), __shfl_xor(s.a, o)}, c);
-  return s;
+  for (int half = kWaves / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (wave < half) {
+      list.merge(s_key[wave + half][lane]);
+      s_key[wave][lane] = list.key;
+    }
+  }
+}
+
+template <int O = 32>
+__device__ __forceinline__ Sums over_lanes(Sums s, float c) {
+  s.add(Sums{lane_xor<O>(s.m), lane_xor<O>(s.s), lane_xor<O>(s.a)}, c);
+  if constexpr (O > 1) return over_lanes<O / 2>(s, c);
+  else return s;
 }
 
 // TOP: a list is wanted.  Rows of one part are done here.
@@ -269,10 +313,9 @@ __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
   using S = Scan<DT, TOP>;
   constexpr int V = S::V, kSize = DT == PILLAR_F32 ? 4 : 2;
   __shared__ Sums s_sums[kWaves];
-  __shared__ float s_x[kWaves][64];
-  __shared__ int s_id[kWaves][64];
+  __shared__ Key s_key[kWaves][64];
   const LogprobArgs& a = p.a;
-  const int r = blockIdx.x / p.parts, part = blockIdx.x - r * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = blockIdx.x / p.parts, part = blockIdx.x - r * p.parts, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Row<DT> row(a, r);
   float given = 0.f;
   bool is_given = false;
@@ -285,25 +328,21 @@ __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
   scan.vectors(reinterpret_cast<const u32x4*>(base + head * kSize), part * p.each, min(whole, (part + 1) * p.each), head, wave);
   if (part == 0 && wave == kWaves - 1) {                 // what is left of the row at both ends, less than 16 logits
     const int id = lane < head ? lane : a.vocab - rest + lane - head;
-    const float x[1] = {lane < head + rest ? logit<DT>(a.logits, row.at + id) : -INFINITY};
+    float x[1] = {lane < head + rest ? logit<DT>(a.logits, row.at + id) : -INFINITY};
     scan.take(x, [&](int) { return id; });
   }
   const Sums sums = over_lanes(scan.sums, p.c);
   if (lane == 0) s_sums[wave] = sums;
-  if (TOP) { s_x[wave][lane] = scan.list.x; s_id[wave][lane] = scan.list.id; }
-  __syncthreads();
+  List list = scan.list;
+  if (TOP) merge_lists(list, s_key, wave, lane);
+  else __syncthreads();
   Sums all = s_sums[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) all.add(s_sums[w], p.c);
-  List list = scan.list;
-  if (TOP && wave == 0) {
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) list.merge(s_x[w][lane], s_id[w][lane]);
-  }
   if (p.parts > 1) {
     const int64_t slot = static_cast<int64_t>(r) * p.parts + part;
     if (tid == 0) *reinterpret_cast<f32x4_t*>(p.msa + 4 * slot) = f32x4_t{all.m, all.s, all.a, 0.f};
-    if (TOP && wave == 0 && lane < a.top) p.lists[slot * a.top + lane] = make_float2(list.x, __int_as_float(list.id));
+    if (TOP && wave == 0 && lane < a.top) p.lists[slot * a.top + lane] = list.key;
     return;
   }
   row.settle(all);
@@ -319,10 +358,9 @@ __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
 template <int DT, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
   __shared__ Sums s_sums[kWaves];
-  __shared__ float s_x[kWaves][64];
-  __shared__ int s_id[kWaves][64];
+  __shared__ Key s_key[kWaves][64];
   const LogprobArgs& a = p.a;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t slot = static_cast<int64_t>(r) * p.parts;
   Row<DT> row(a, r);
   float given = 0.f;
@@ -336,17 +374,27 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
   sums = over_lanes(sums, p.c);
   if (lane == 0) s_sums[wave] = sums;
   List list;
-  list.clear();
   if (TOP) {
-    for (int i = wave; i < p.parts; i += kWaves) {
-      float2 v = make_float2(-INFINITY, __int_as_float(kNoId));
-      if (lane < a.top) v = p.lists[(slot + i) * a.top + lane];
-      list.merge(v.x, __float_as_int(v.y));
+    constexpr int kLists = 8;                            // lists on their way at once
+    for (int i = wave; i < p.parts; i += kLists * kWaves) {
+      Key v[kLists];
+#pragma unroll
+      for (int k = 0; k < kLists; ++k) {
+        v[k] = 0;
+        if (i + k * kWaves < p.parts && lane < a.top) v[k] = p.lists[(slot + i + k * kWaves) * a.top + lane];
+      }
+#pragma unroll 1
+      for (int k = 0; k < kLists; ++k) {
+        if (i + k * kWaves >= p.parts) break;
+        list.merge(v[0]);
+#pragma unroll
+        for (int l = 0; l + 1 < kLists; ++l) v[l] = v[l + 1];
+      }
     }
-    s_x[wave][lane] = list.x;
-    s_id[wave][lane] = list.id;
+    merge_lists(list, s_key, wave, lane);
+  } else {
+    __syncthreads();
   }
-  __syncthreads();
   sums = s_sums[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sums.add(s_sums[w], p.c);
@@ -357,10 +405,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
     is_given = row.given(j, given);
     row.put(j, is_given, given);
   }
-  if (!TOP || wave > 0) return;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) list.merge(s_x[w][lane], s_id[w][lane]);
-  row.put_list(list);
+  if (TOP && wave == 0) row.put_list(list);
 }
 
 struct Plan {
@@ -406,7 +451,7 @@ hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
   p.parts = plan.parts;
   p.each = plan.each;
   p.msa = static_cast<float*>(a.workspace);
-  p.lists = reinterpret_cast<float2*>(static_cast<char*>(a.workspace) + align_up(static_cast<size_t>(a.rows) * plan.parts * 16, 256));
+  p.lists = reinterpret_cast<Key*>(static_cast<char*>(a.workspace) + align_up(static_cast<size_t>(a.rows) * plan.parts * 16, 256));
   if (a.dtype == PILLAR_F32) return a.top ? launch<PILLAR_F32, true>(p, s) : launch<PILLAR_F32, false>(p, s);
   return a.top ? launch<PILLAR_BF16, true>(p, s) : launch<PILLAR_BF16, false>(p, s);
 }
