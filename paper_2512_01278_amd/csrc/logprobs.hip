@@ -126,13 +126,14 @@ struct Scan {
   // they are few, else sorted and merged at once.
   template <int N, typename Id>
   __device__ __forceinline__ void enter(float (&x)[N], Id id, float most) {
-    do {
+    while (true) {
       int at = 0;
 #pragma unroll
       for (int i = N - 1; i > 0; --i) at = x[i] == most ? i : at;
       if (x[0] == most) at = 0;
       const Key mine = most >= least && most > -INFINITY ? key_of(most, id(at)) : 0;
       uint64_t some = __ballot(mine > least_key);
+      if (!some) return;                                 // (a logit equal to the list's last gets in where its number is lower)
       if (__builtin_popcountll(some) > kFew) {
         List sorted;
         sorted.key = mine;
@@ -154,11 +155,11 @@ struct Scan {
       most = x[0];
 #pragma unroll
       for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
-    } while (__any(most > least));
+    }
   }
 
-  // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th
-  template <int N, typename Id>
+  // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th.  LATER: all of them higher than those before.
+  template <bool LATER, int N, typename Id>
   __device__ __forceinline__ void take(float (&x)[N], Id id) {
     float most = x[0];
 #pragma unroll
@@ -179,7 +180,7 @@ struct Scan {
     sums.s += s[0] + s[1];
     sums.a += a[0] + a[1];
     if constexpr (TOP) {
-      if (__any(most > least)) enter(x, id, most);
+      if (__any(LATER ? most > least : most >= least)) enter(x, id, most);
     }
   }
 
@@ -213,7 +214,7 @@ struct Scan {
 #pragma unroll
           for (int i = 0; i < kBatch; ++i) x[i] = v + 64 * (i / V) + lane < v1 ? x[i] : -INFINITY;
         }
-        take(x, [&](int i) { return first + (v + 64 * (i / V) + lane) * V + i % V; });          // (V is a power of two)
+        take<true>(x, [&](int i) { return first + (v + 64 * (i / V) + lane) * V + i % V; });          // (V is a power of two)
         v += kNext;
         if (v >= v1) return;
       }
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
   if (part == 0 && wave == kWaves - 1) {                 // what is left of the row at both ends, less than 16 logits
     const int id = lane < head ? lane : a.vocab - rest + lane - head;
     float x[1] = {lane < head + rest ? logit<DT>(a.logits, row.at + id) : -INFINITY};
-    scan.take(x, [&](int) { return id; });
+    scan.template take<false>(x, [&](int) { return id; });
   }
   const Sums sums = over_lanes(scan.sums, p.c);
   if (lane == 0) s_sums[wave] = sums;
