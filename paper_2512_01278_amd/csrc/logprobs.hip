@@ -385,8 +385,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
         if (i + k * kWaves < p.parts && lane < a.top) v[k] = p.lists[(slot + i + k * kWaves) * a.top + lane];
       }
 #pragma unroll 1
-      for (int k = 0; k < kLists; ++k) {
-        if (i + k * kWaves >= p.parts) break;
+      for (int k = 0; k < kLists && i + k * kWaves < p.parts; ++k) {     // (one copy of the code)
         list.merge(v[0]);
 #pragma unroll
         for (int l = 0; l + 1 < kLists; ++l) v[l] = v[l + 1];

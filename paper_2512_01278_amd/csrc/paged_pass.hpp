@@ -47,11 +47,13 @@ struct Ranges {
 struct Share {
   int w, u0, u1;               // its range, first unit and past the last
   int b, ub;                   // the request that has unit u0, and that request's first unit
+  int total;                   // units of the launch
   // units: of a request; each(c): called for every 64 requests; prefix: the first workgroup leaves the units before every request, and all of them, there
   template <typename F, typename Each>
   __device__ __forceinline__ Share(int batch, int workgroups, int few, int tiles8, int32_t* prefix, F units, Each each) {
     const int lane = threadIdx.x & 63;
-    int total = 0, mine = 0, upto = 0;
+    int mine = 0, upto = 0;
+    total = 0;
     for (int c = 0; c < batch; c += 64) {
       mine = c + lane < batch ? units(c + lane) : 0;
       upto = total + wave_inclusive(mine);

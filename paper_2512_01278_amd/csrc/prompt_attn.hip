@@ -19,6 +19,15 @@
 namespace pillar {
 namespace {
 
+// What a range says about the tile that it begins in, for the joining of its partials.
+struct Cut {
+  int first, steps;            // the tile's first unit, its units
+  int row;                     // the packed row of its first token
+  int rows, head;              // rows of the tile (tokens times group), first query head
+  int pad[3];
+};
+static_assert(sizeof(Cut) == 32, "");
+
 struct PromptParams {
   KvView kv;
   const void* q;
@@ -26,10 +35,13 @@ struct PromptParams {
   void* out;
   float* lse;                  // may be null
   int32_t total_rows, max_new, group, q_dtype, q_shift;
+  int32_t part_rows;           // rows that a partial result has room for
+  int32_t setup;               // units that a tile counts for beside its steps
   bool aligned;                // cache rows can be read 16 bytes at a time,
   bool dense;                  // rows of q and out too
   // workspace
-  int32_t* prefix;             // [B+1] units before a request, and all of them
+  int32_t* total;              // units of the launch
+  Cut* cuts;                   // [ranges]
   float* part_ml;              // [slots][RT][2]
   float* part_o;               // [slots][RT][D]
   int32_t ranges, few;         // workgroups of the pass; of those, with little to do
@@ -46,8 +58,15 @@ struct Request {
     len = min(max(a.kv.seq_lens[b], 0), a.kv.max_seq_len);
   }
 };
-template <int TS>
-__device__ __forceinline__ PromptSteps steps_of(const PromptParams& a, const Request& r) { return PromptSteps(r.len, r.n, a.q_shift, shift_of(TS)); }
+// A request with few rows (single tokens, a chain) among prompts is read in larger steps, by a workgroup whose wavefronts share the rows: in 64 tokens at a time its
+// one wavefront with rows would keep the others waiting.  A step then takes about as long as one of 256 rows, so ranges stay even.  31 single tokens after
+// 1-8 K beside a chunk of 1000: 268 / 214 us (with steps of 256 tokens, twice as long as the others, 265).
+constexpr int kNarrowRows = 64;
+__device__ __forceinline__ bool is_narrow(const PromptParams& a, const Request& r) { return r.n * a.group <= kNarrowRows; }
+template <typename C, typename N>
+__device__ __forceinline__ PromptSteps steps_of(const PromptParams& a, const Request& r) {
+  return PromptSteps(r.len, r.n, a.q_shift, is_narrow(a, r) ? shift_of(N::TS) : shift_of(C::TS), a.setup);
+}
 
 // four dims of an output row
 __device__ __forceinline__ void store_four(const PromptParams& a, int64_t at, f32x4 x) {
@@ -60,10 +79,8 @@ __device__ __forceinline__ void store_four(const PromptParams& a, int64_t at, f3
     for (int j = 0; j < 4; ++j) Storage<PILLAR_F32>::store(a.out, at + j, x[j]);
   } else {
     if (a.dense) {
-      u32x2 y;
-      y.x = f32_to_bf16(x[0]) | static_cast<uint32_t>(f32_to_bf16(x[1])) << 16;
-      y.y = f32_to_bf16(x[2]) | static_cast<uint32_t>(f32_to_bf16(x[3])) << 16;
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = y;
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(a.out) + at) = __builtin_convertvector(x, bf16x4);
       return;
     }
 #pragma unroll
@@ -85,303 +102,336 @@ __device__ __forceinline__ void see_nothing(const PromptParams& a, const Request
 // Of 32 tokens, those that a row sees which sees `upto` of them (any number).
 __device__ __forceinline__ uint32_t first_tokens(int upto) { return upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1; }
 
+// A stretch: steps s0 .. s1 - 1 of a tile.
+struct Stretch {
+  int b, g, s0, s1;
+  int i0, rows;                // the tile's first new token, its rows
+  int slot;                    // of the partial result
+  bool whole;                  // it is all of the tile
+};
+
 template <typename C>
-__global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void prompt_pass(PromptParams a) {
+struct PassLds {
+  uint8_t* smem;
+  float *ks, *log_vs, *inv_vs;                           // page scales of a step's tokens: k_scale in the logits' unit, log2 of v_scale, and one over it
+  float (*m)[32], (*l)[32];
+  uint32_t (*bad)[8];                                    // the tile's own tokens whose V row is not finite throughout; two sets, cleared in turn
+};
+
+template <typename C>
+__device__ __forceinline__ void do_stretch(const PromptParams& a, const Stretch& st, const Request& rq, const PassLds<C>& lds, int parity) {
   using E = typename C::E;
   constexpr int D = C::D, TS = C::TS, RT = C::RT;
   constexpr int kBadWords = RT / 32;                     // a tile has at most RT tokens
-  __shared__ __attribute__((aligned(16))) uint8_t smem[C::kLds];
-  // page scales of the tile's tokens: k_scale in the logits' unit, log2 of v_scale, and one over it
-  __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? TS : 4], s_log_vs[C::kScales ? TS : 4], s_inv_vs[C::kScales ? TS : 4];
-  __shared__ float s_m[C::kWaves][32], s_l[C::kWaves][32];
-  __shared__ uint32_t s_bad[2][kBadWords];               // the tile's own tokens whose V row is not finite throughout
   const KvView& kv = a.kv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % C::WR, wt = wave / C::WR;
   const int n = lane & 31, g2 = lane >> 5;
-  uint8_t* const ktile = smem;
-  uint8_t* const vtile = smem + TS * E::kKPitch;
+  uint8_t* const ktile = lds.smem;
+  uint8_t* const vtile = lds.smem + TS * E::kKPitch;
   const float scale2 = kv.sm_scale * kLog2e;
   const float unit = C::kScales ? 1.f : scale2;          // of the logits, in log2: page scales come with it
+  const int b = st.b, g = st.g, s0 = st.s0, s1 = st.s1, i0 = st.i0, rows = st.rows;
 
-  const Share share(kv.batch, a.ranges, a.few, a.tiles8, a.prefix,
-                    [&](int r) { return steps_of<TS>(a, Request(a, r)).units() * kv.num_kv_heads; }, [&](int c) {
+  Carrier<C, true> c(kv, b, g, rq.len);                // (first of all: the rows of the cache are at the end of a chain of three loads)
+  c.pages(kv, s0);
+
+  // ---- rows ----
+  const int first = rq.len - rq.n;                     // number of the first new token (below 0: it is not in the cache)
+  const int row = wr * 32 + n;
+  const bool there = row < rows, any_row = wr * 32 < rows;
+  const int token = i0 + (there ? row / a.group : 0), head = g * a.group + (there ? row % a.group : 0);
+  const int64_t out_row = static_cast<int64_t>(rq.row0 + token) * kv.num_q_heads + head;
+  typename E::Query qf;
+  E::load_query(qf, a.q, out_row, there, a.q_dtype, a.dense, g2);
+  const int sees = there ? first + token + 1 : 0;      // tokens that this row sees
+  const int wave_sees0 = first + i0 + wr * 32 / a.group + 1;                                // ... the wavefront's first row, its last
+  const int wave_sees1 = first + i0 + (min(wr * 32 + 32, rows) - 1) / a.group + 1;
+  const int own = max(first + i0, 0);                  // first of the tile's own tokens, which not all rows see
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  c.fetch(kv, g, s0, a.aligned);
+  if (s0 + 1 < s1) c.pages(kv, s0 + 1);
+
+  // What is not finite in V of one of the tile's own tokens counts for the rows that see it only: it is left out of the tile, and added at the end.
+  auto park_v = [&](const u32x4& x, float scale, int s, int r, int piece, bool tail) {
+    uint8_t* to = vtile + r * E::kVPitch;
+    const int t = s * TS + r;
+    if (!tail || t < own) {
+      park_piece<E, C::KV, false>(x, scale, to, piece);
+    } else if (park_piece<E, C::KV, true>(x, scale, to, piece) && t - own < RT) {
+      atomicOr(&lds.bad[parity][(t - own) >> 5], 1u << ((t - own) & 31));
+    }
+  };
+
+  for (int s = s0; s < s1; ++s) {
+    const bool tail = (s + 1) * TS > own;              // some token of the step is the tile's own, or later
+    // ---- the step's rows into LDS, the next ones on their way ----
+    if (c.carries()) {
+#pragma unroll
+      for (int i = 0; i < C::kLoads; ++i) {
+        park_piece<E, C::KV, false>(c.k[i], c.k_scale(i), ktile + c.row(i) * E::kKPitch, c.piece);
+        park_v(c.v[i], c.v_scale(i), s, c.row(i), c.piece, tail);
+      }
+    }
+    if (C::kScales && tid < TS) {                      // (v_scale in the exponent: the weightiest token of a row is not rounded)
+      const float log_vs = __builtin_amdgcn_logf(c.vs < kLeastScale ? kLeastScale : c.vs);
+      lds.ks[tid] = c.ks * scale2;
+      lds.log_vs[tid] = log_vs;
+      lds.inv_vs[tid] = fast_exp2(-log_vs);              // (of the rounded logarithm: l is exact to fp32)
+    }
+    __syncthreads();
+    if (s + 1 < s1) {
+      c.fetch(kv, g, s + 1, a.aligned);
+      if (s + 2 < s1) c.pages(kv, s + 2);
+    }
+    if (s == s0 && tid < 8) lds.bad[parity ^ 1][tid] = 0;
+
+    const int at = wt * C::kGroupTokens, t0 = s * TS + at;
+    if (any_row && t0 < wave_sees1) {
+      if (C::WR == 4) __builtin_amdgcn_s_setprio(1);
+      const bool masked = t0 + C::kGroupTokens > wave_sees0;
+      f32x16 x[C::NS];
+#pragma unroll
+      for (int sub = 0; sub < C::NS; ++sub) {
+        x[sub] = E::qk(ktile + (at + 32 * sub) * E::kKPitch, qf, lane);
+        if constexpr (C::kScales) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const f32x4 f = *reinterpret_cast<const f32x4*>(lds.ks + at + 32 * sub + elem_of(i, g2));
+            const f32x4 d = *reinterpret_cast<const f32x4*>(lds.log_vs + at + 32 * sub + elem_of(i, g2));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[sub][i + j] = __builtin_fmaf(x[sub][i + j], f[j], d[j]);
+          }
+        }
+      }
+      uint32_t seen[C::NS];                            // bit elem_of(i, 0): this row sees the token of element i
+      if (masked) {
+#pragma unroll
+        for (int sub = 0; sub < C::NS; ++sub) {
+          seen[sub] = first_tokens(sees - t0 - 32 * sub) >> (4 * g2);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[sub][i] = (seen[sub] >> elem_of(i, 0) & 1u) ? x[sub][i] : -INFINITY;
+        }
+      }
+      float top = x[0][0];
+#pragma unroll
+      for (int sub = 0; sub < C::NS; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[sub][i]);
+      top = other_half_max(top) * unit;
+      // the maximum moves only when a logit exceeds it by more than 8 (log2): P stays below 2^8, and the accumulators are rescaled a few times per stretch
+      const bool moves = top > m_run + 8.f;
+      if (__any(moves)) {
+        const float f = !moves ? 1.f : m_run == -INFINITY ? 0.f : fast_exp2(m_run - top);
+        m_run = moves ? top : m_run;
+        l_run *= f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= f;
+      }
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int sub = 0; sub < C::NS; ++sub) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[sub][i] = fast_exp2(C::kScales ? x[sub][i] - m_use : __builtin_fmaf(x[sub][i], scale2, -m_use));
+          if (!C::kScales) sum[i & 1] += x[sub][i];
+        }
+        if constexpr (C::kScales) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const f32x4 f = *reinterpret_cast<const f32x4*>(lds.inv_vs + at + 32 * sub + elem_of(i, g2));
+            if (masked) {                              // (the scale of a page that no row sees may be anything)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sum[j & 1] += (seen[sub] >> elem_of(i + j, 0) & 1u) ? x[sub][i + j] * f[j] : 0.f;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sum[j & 1] = __builtin_fmaf(x[sub][i + j], f[j], sum[j & 1]);
+            }
+          }
+        }
+        E::pv(vtile + (at + 32 * sub) * E::kVPitch, x[sub], o, lane);
+      }
+      l_run += sum[0] + sum[1];
+      if (C::WR == 4) __builtin_amdgcn_s_setprio(0);
+    }
+    __syncthreads();
+  }
+
+  const uint32_t bad = lane < kBadWords ? lds.bad[parity][lane] : 0;
+  for (uint64_t some = __ballot(bad != 0); some; some &= some - 1) {
+    const int word = __builtin_ctzll(some);
+    for (uint32_t left = __builtin_amdgcn_readlane(bad, word); left; left &= left - 1) {
+      const int t = own + 32 * word + __builtin_ctz(left);
+      if (t >= rq.len) break;                          // (there is no such row)
+      if ((t % TS) / C::kGroupTokens != wt) continue;  // (the wavefronts whose maximum has seen the token)
+      int page;
+      const int64_t from = row_offset(kv, b, g, t, &page);
+      float vs = 1.f;
+      if constexpr (C::KV == PILLAR_FP8_E4M3) vs = kv.v_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float val = Storage<C::KV>::load(kv.v_pool, from + 32 * db + elem_of(i, g2)) * vs;
+          const float was = val;
+          if (drop_nonfinite(val) && t < sees) o[db][i] += was;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
+
+  // ---- what the stretch leaves ----
+  l_run = other_half_sum(l_run);
+  auto leave_row = [&](int64_t to_row, int in_tile, float m, float l) {        // one lane per row
+    if (st.whole) {
+      if (a.lse) a.lse[to_row] = (l == 0.f ? -INFINITY : m + log2f(l)) * kLn2;
+    } else {
+      float* ml = a.part_ml + (static_cast<int64_t>(st.slot) * a.part_rows + in_tile) * 2;
+      ml[0] = m;
+      ml[1] = l;
+    }
+  };
+  auto leave_dims = [&](int64_t to_row, int in_tile, int dim, f32x4 x, float inv) {
+    if (!st.whole) *reinterpret_cast<f32x4*>(a.part_o + (static_cast<int64_t>(st.slot) * a.part_rows + in_tile) * D + dim) = x;
+    else store_four(a, to_row * D + dim, x * inv);
+  };
+  if constexpr (C::WT == 1) {
+    if (there) {
+      if (g2 == 0) leave_row(out_row, row, m_run, l_run);
+      const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          leave_dims(out_row, row, 32 * db + elem_of(i, g2), f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]}, inv);
+    }
+  } else {
+    // the wavefronts that shared the rows join in LDS, where the step's rows were
+    float* join = reinterpret_cast<float*>(lds.smem);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4*>(join + (wave * 32 + n) * C::kJoinRow + 32 * db + elem_of(i, g2)) = f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
+    if (g2 == 0) { lds.m[wave][n] = m_run; lds.l[wave][n] = l_run; }
+    __syncthreads();
+    constexpr int kQuads = D / 4;
+    for (int e = tid; e < RT * kQuads; e += C::kThreads) {
+      const int r = e / kQuads, dim = 4 * (e % kQuads);
+      if (r >= rows) continue;
+      float m = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < C::WT; ++k) m = fmaxf(m, lds.m[k * C::WR + (r >> 5)][r & 31]);
+      const float m_use = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+      f32x4 x = {};
+#pragma unroll
+      for (int k = 0; k < C::WT; ++k) {
+        const int from = k * C::WR + (r >> 5);
+        const float f = fast_exp2(lds.m[from][r & 31] - m_use);
+        l += lds.l[from][r & 31] * f;
+        x += *reinterpret_cast<const f32x4*>(join + (from * 32 + (r & 31)) * C::kJoinRow + dim) * f;
+      }
+      const int64_t to = static_cast<int64_t>(rq.row0 + i0 + r / a.group) * kv.num_q_heads + g * a.group + r % a.group;
+      if (dim == 0) leave_row(to, r, m, l);
+      leave_dims(to, r, dim, x, l == 0.f ? 0.f : 1.f / l);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename C, typename N>
+__global__ __launch_bounds__(C::kThreads, C::E::kF32 ? 1 : 2) void prompt_pass(PromptParams a) {
+  static_assert(C::kThreads == N::kThreads && (std::is_same_v<C, N> || N::RT >= kNarrowRows), "");
+  constexpr int kTokens = C::TS > N::TS ? C::TS : N::TS;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[C::kLds > N::kLds ? C::kLds : N::kLds];
+  __shared__ __attribute__((aligned(16))) float s_ks[C::kScales ? kTokens : 4], s_log_vs[C::kScales ? kTokens : 4], s_inv_vs[C::kScales ? kTokens : 4];
+  __shared__ float s_m[C::kWaves][32], s_l[C::kWaves][32];
+  __shared__ uint32_t s_bad[2][8];
+  const KvView& kv = a.kv;
+  const int tid = threadIdx.x, lane = tid & 63;
+
+  const Share share(kv.batch, a.ranges, a.few, a.tiles8, nullptr,
+                    [&](int r) { return steps_of<C, N>(a, Request(a, r)).units() * kv.num_kv_heads; }, [&](int c) {
     // requests without a token in the cache have no unit: their rows are shared out among the workgroups
     for (uint64_t none = __ballot(c + lane < kv.batch && kv.seq_lens[min(c + lane, kv.batch - 1)] <= 0); none; none &= none - 1) {
       const int r = c + __builtin_ctzll(none);
       if (r % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) see_nothing(a, Request(a, r));
     }
   });
-  int b = share.b, ub = share.ub;                        // the request at work and its first unit
   const int w = share.w, u0 = share.u0, u1 = share.u1;
+  if (blockIdx.x == 0 && tid == 0) *a.total = share.total;
   if (u0 == u1) return;
-  if (tid < kBadWords) s_bad[0][tid] = 0;
+  if (tid < 8) s_bad[0][tid] = 0;
   int parity = 0;              // of the stretch: the other half of s_bad is cleared meanwhile
   __syncthreads();
 
+  // the request at work, its first unit and its units
+  int b = share.b, ub = share.ub;
+  Request rq(a, b);
+  PromptSteps plan = steps_of<C, N>(a, rq);
+  int per_head = plan.units();
   for (int u = u0; u < u1;) {
-    b = __builtin_amdgcn_readfirstlane(b);
-    const Request rq(a, b);
-    const PromptSteps plan = steps_of<TS>(a, rq);
-    const int per_head = plan.units(), units = per_head * kv.num_kv_heads;
-    if (u >= ub + units) {     // (a request without units among them)
-      ub += units;
-      ++b;
-      continue;
+    while (u >= ub + per_head * kv.num_kv_heads) {       // (requests without units among them)
+      ub += per_head * kv.num_kv_heads;
+      b = __builtin_amdgcn_readfirstlane(b + 1);
+      rq = Request(a, b);
+      plan = steps_of<C, N>(a, rq);
+      per_head = plan.units();
     }
-    const int rel = u - ub, g = rel / per_head, in_head = rel - g * per_head;
+    Stretch st;
+    const int rel = u - ub, in_head = rel % per_head;
     const int tile = __builtin_amdgcn_readfirstlane(plan.tile_of(in_head));
-    const int steps = plan.steps(tile), s0 = in_head - static_cast<int>(plan.before(tile));
-    const int s1 = min(steps, s0 + (u1 - u));
-    const bool whole = s0 == 0 && s1 == steps;
-    const int slot = 2 * w + (u == u0 ? 0 : 1);
-    u += s1 - s0;
-
-    // ---- rows ----
-    const int first = rq.len - rq.n;                     // number of the first new token (below 0: it is not in the cache)
-    const int i0 = tile << a.q_shift, rows = min(rq.n - i0, 1 << a.q_shift) * a.group;        // the tile's first new token, its rows
-    const int row = wr * 32 + n;
-    const bool there = row < rows, any_row = wr * 32 < rows;
-    const int token = i0 + (there ? row / a.group : 0), head = g * a.group + (there ? row % a.group : 0);
-    const int64_t out_row = static_cast<int64_t>(rq.row0 + token) * kv.num_q_heads + head;
-    typename E::Query qf;
-    E::load_query(qf, a.q, out_row, there, a.q_dtype, a.dense, g2);
-    const int sees = there ? first + token + 1 : 0;      // tokens that this row sees
-    const int wave_sees0 = first + i0 + wr * 32 / a.group + 1;                                // ... the wavefront's first row, its last
-    const int wave_sees1 = first + i0 + (min(wr * 32 + 32, rows) - 1) / a.group + 1;
-    const int own = max(first + i0, 0);                  // first of the tile's own tokens, which not all rows see
-    f32x16 o[D / 32];
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
-    float m_run = -INFINITY, l_run = 0.f;
-
-    Carrier<C, true> c(kv, b, g, rq.len);
-    c.pages(kv, s0);
-    c.fetch(kv, g, s0, a.aligned);
-    if (s0 + 1 < s1) c.pages(kv, s0 + 1);
-
-    // What is not finite in V of one of the tile's own tokens counts for the rows that see it only: it is left out of the tile, and added at the end.
-    auto park_v = [&](const u32x4& x, float scale, int s, int r, int piece, bool tail) {
-      uint8_t* to = vtile + r * E::kVPitch;
-      const int t = s * TS + r;
-      if (!tail || t < own) {
-        park_piece<E, C::KV, false>(x, scale, to, piece);
-      } else if (park_piece<E, C::KV, true>(x, scale, to, piece) && t - own < RT) {
-        atomicOr(&s_bad[parity][(t - own) >> 5], 1u << ((t - own) & 31));
-      }
-    };
-
-    for (int s = s0; s < s1; ++s) {
-      const bool tail = (s + 1) * TS > own;              // some token of the step is the tile's own, or later
-      // ---- the step's rows into LDS, the next ones on their way ----
-      if (c.carries()) {
-#pragma unroll
-        for (int i = 0; i < C::kLoads; ++i) {
-          park_piece<E, C::KV, false>(c.k[i], c.k_scale(i), ktile + c.row(i) * E::kKPitch, c.piece);
-          park_v(c.v[i], c.v_scale(i), s, c.row(i), c.piece, tail);
-        }
-      }
-      if (C::kScales && tid < TS) {                      // (v_scale in the exponent: the weightiest token of a row is not rounded)
-        const float log_vs = __builtin_amdgcn_logf(c.vs < kLeastScale ? kLeastScale : c.vs);
-        s_ks[tid] = c.ks * scale2;
-        s_log_vs[tid] = log_vs;
-        s_inv_vs[tid] = fast_exp2(-log_vs);              // (of the rounded logarithm: l is exact to fp32)
-      }
-      __syncthreads();
-      if (s + 1 < s1) {
-        c.fetch(kv, g, s + 1, a.aligned);
-        if (s + 2 < s1) c.pages(kv, s + 2);
-      }
-      if (s == s0 && tid < kBadWords) s_bad[parity ^ 1][tid] = 0;
-
-      const int at = wt * C::kGroupTokens, t0 = s * TS + at;
-      if (any_row && t0 < wave_sees1) {
-        if (C::WR == 4) __builtin_amdgcn_s_setprio(1);
-        const bool masked = t0 + C::kGroupTokens > wave_sees0;
-        f32x16 x[C::NS];
-#pragma unroll
-        for (int sub = 0; sub < C::NS; ++sub) {
-          x[sub] = E::qk(ktile + (at + 32 * sub) * E::kKPitch, qf, lane);
-          if constexpr (C::kScales) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(s_ks + at + 32 * sub + elem_of(i, g2));
-              const f32x4 d = *reinterpret_cast<const f32x4*>(s_log_vs + at + 32 * sub + elem_of(i, g2));
-#pragma unroll
-              for (int j = 0; j < 4; ++j) x[sub][i + j] = __builtin_fmaf(x[sub][i + j], f[j], d[j]);
-            }
-          }
-        }
-        uint32_t seen[C::NS];                            // bit elem_of(i, 0): this row sees the token of element i
-        if (masked) {
-#pragma unroll
-          for (int sub = 0; sub < C::NS; ++sub) {
-            seen[sub] = first_tokens(sees - t0 - 32 * sub) >> (4 * g2);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[sub][i] = (seen[sub] >> elem_of(i, 0) & 1u) ? x[sub][i] : -INFINITY;
-          }
-        }
-        float top = x[0][0];
-#pragma unroll
-        for (int sub = 0; sub < C::NS; ++sub)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, x[sub][i]);
-        top = other_half_max(top) * unit;
-        // the maximum moves only when a logit exceeds it by more than 8 (log2): P stays below 2^8, and the accumulators are rescaled a few times per stretch
-        const bool moves = top > m_run + 8.f;
-        if (__any(moves)) {
-          const float f = !moves ? 1.f : m_run == -INFINITY ? 0.f : fast_exp2(m_run - top);
-          m_run = moves ? top : m_run;
-          l_run *= f;
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[db][i] *= f;
-        }
-        const float m_use = m_run == -INFINITY ? 0.f : m_run;
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int sub = 0; sub < C::NS; ++sub) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            x[sub][i] = fast_exp2(C::kScales ? x[sub][i] - m_use : __builtin_fmaf(x[sub][i], scale2, -m_use));
-            if (!C::kScales) sum[i & 1] += x[sub][i];
-          }
-          if constexpr (C::kScales) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(s_inv_vs + at + 32 * sub + elem_of(i, g2));
-              if (masked) {                              // (the scale of a page that no row sees may be anything)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j & 1] += (seen[sub] >> elem_of(i + j, 0) & 1u) ? x[sub][i + j] * f[j] : 0.f;
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j & 1] = __builtin_fmaf(x[sub][i + j], f[j], sum[j & 1]);
-              }
-            }
-          }
-          E::pv(vtile + (at + 32 * sub) * E::kVPitch, x[sub], o, lane);
-        }
-        l_run += sum[0] + sum[1];
-        if (C::WR == 4) __builtin_amdgcn_s_setprio(0);
-      }
-      __syncthreads();
+    const int steps = plan.steps(tile), idx = in_head - plan.before(tile), units = steps + a.setup;
+    st.b = b;
+    st.g = rel / per_head;
+    st.s0 = max(0, idx - a.setup);
+    st.s1 = min(units, idx + (u1 - u)) - a.setup;        // (0 or less: the range ends before the tile's first step)
+    st.whole = st.s0 == 0 && st.s1 == steps;
+    st.slot = 2 * w + (u == u0 ? 0 : 1);
+    st.i0 = tile << a.q_shift;
+    st.rows = min(rq.n - st.i0, 1 << a.q_shift) * a.group;
+    if (u == u0 && tid == 0) {
+      Cut cut{};
+      cut.first = u - idx;
+      cut.steps = steps;
+      cut.row = rq.row0 + st.i0;
+      cut.rows = st.rows;
+      cut.head = st.g * a.group;
+      a.cuts[w] = cut;
     }
-
-    for (int word = 0; word < kBadWords; ++word) {
-      for (uint32_t left = __builtin_amdgcn_readfirstlane(s_bad[parity][word]); left; left &= left - 1) {
-        const int t = own + 32 * word + __builtin_ctz(left);
-        if (t >= rq.len) break;                          // (there is no such row)
-        if ((t % TS) / C::kGroupTokens != wt) continue;  // (the wavefronts whose maximum has seen the token)
-        int page;
-        const int64_t from = row_offset(kv, b, g, t, &page);
-        float vs = 1.f;
-        if constexpr (C::KV == PILLAR_FP8_E4M3) vs = kv.v_scale[static_cast<int64_t>(page) * kv.num_kv_heads + g];
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float val = Storage<C::KV>::load(kv.v_pool, from + 32 * db + elem_of(i, g2)) * vs;
-            const float was = val;
-            if (drop_nonfinite(val) && t < sees) o[db][i] += was;
-            __builtin_amdgcn_sched_barrier(0);
-          }
-      }
-    }
+    u += min(units - idx, u1 - u);
+    if (st.s1 <= 0) break;
+    if constexpr (std::is_same_v<C, N>) do_stretch<C>(a, st, rq, PassLds<C>{smem, s_ks, s_log_vs, s_inv_vs, s_m, s_l, s_bad}, parity);
+    else if (is_narrow(a, rq)) do_stretch<N>(a, st, rq, PassLds<N>{smem, s_ks, s_log_vs, s_inv_vs, s_m, s_l, s_bad}, parity);
+    else do_stretch<C>(a, st, rq, PassLds<C>{smem, s_ks, s_log_vs, s_inv_vs, s_m, s_l, s_bad}, parity);
     parity ^= 1;
-
-    // ---- what the stretch leaves ----
-    l_run = other_half_sum(l_run);
-    auto leave_row = [&](int64_t to_row, int in_tile, float m, float l) {        // one lane per row
-      if (whole) {
-        if (a.lse) a.lse[to_row] = (l == 0.f ? -INFINITY : m + log2f(l)) * kLn2;
-      } else {
-        float* ml = a.part_ml + (static_cast<int64_t>(slot) * RT + in_tile) * 2;
-        ml[0] = m;
-        ml[1] = l;
-      }
-    };
-    auto leave_dims = [&](int64_t to_row, int in_tile, int dim, f32x4 x, float inv) {
-      if (!whole) *reinterpret_cast<f32x4*>(a.part_o + (static_cast<int64_t>(slot) * RT + in_tile) * D + dim) = x;
-      else store_four(a, to_row * D + dim, x * inv);
-    };
-    if constexpr (C::WT == 1) {
-      if (there) {
-        if (g2 == 0) leave_row(out_row, row, m_run, l_run);
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            leave_dims(out_row, row, 32 * db + elem_of(i, g2), f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]}, inv);
-      }
-    } else {
-      // the wavefronts that shared the rows join in LDS, where the step's rows were
-      float* join = reinterpret_cast<float*>(smem);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(join + (wave * 32 + n) * C::kJoinRow + 32 * db + elem_of(i, g2)) = f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
-      if (g2 == 0) { s_m[wave][n] = m_run; s_l[wave][n] = l_run; }
-      __syncthreads();
-      constexpr int kQuads = D / 4;
-      for (int e = tid; e < RT * kQuads; e += C::kThreads) {
-        const int r = e / kQuads, dim = 4 * (e % kQuads);
-        if (r >= rows) continue;
-        float m = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < C::WT; ++k) m = fmaxf(m, s_m[k * C::WR + (r >> 5)][r & 31]);
-        const float m_use = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        f32x4 x = {};
-#pragma unroll
-        for (int k = 0; k < C::WT; ++k) {
-          const int from = k * C::WR + (r >> 5);
-          const float f = fast_exp2(s_m[from][r & 31] - m_use);
-          l += s_l[from][r & 31] * f;
-          x += *reinterpret_cast<const f32x4*>(join + (from * 32 + (r & 31)) * C::kJoinRow + dim) * f;
-        }
-        const int64_t to = static_cast<int64_t>(rq.row0 + i0 + r / a.group) * kv.num_q_heads + g * a.group + r % a.group;
-        if (dim == 0) leave_row(to, r, m, l);
-        leave_dims(to, r, dim, x, l == 0.f ? 0.f : 1.f / l);
-      }
-      __syncthreads();
-    }
   }
 }
 
 // ---- joins what several ranges left of a tile.  A tile is cut where a range begins inside it, so there is a row of workgroups for each range, which
 // do nothing unless theirs is the first to begin inside its tile.  A row has D/4 lanes: they fetch (m, l) of as many partials side by
 // side, and the partials of O kAhead at a time. ----
-template <int D, int TS, int RT, int kAhead>
+template <int D, int RT, int kAhead>
 __global__ __launch_bounds__(128) void prompt_merge(PromptParams a) {
   constexpr int kLanes = D / 4, kRows = 128 / kLanes;
-  const KvView& kv = a.kv;
-  const int lane = threadIdx.x & 63, part = threadIdx.x % kLanes;
-  const Ranges ranges(a.prefix[kv.batch], a.ranges, a.few, a.tiles8);
+  const int part = threadIdx.x % kLanes;
   const int w = blockIdx.x + 1;
+  const Ranges ranges(*a.total, a.ranges, a.few, a.tiles8);
   if (w >= ranges.n) return;
-  const int u = ranges.begin(w);
-  int b = 0;
-  for (int c = 0; c < kv.batch; c += 64) {
-    const uint64_t after = __ballot(c + lane < kv.batch && a.prefix[min(c + lane, kv.batch - 1) + 1] > u);
-    if (after) {
-      b = c + __builtin_ctzll(after);
-      break;
-    }
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
-  const Request rq(a, b);
-  const PromptSteps plan = steps_of<TS>(a, rq);
-  const int ub = a.prefix[b], per_head = plan.units(), g = (u - ub) / per_head, in_head = u - ub - g * per_head;
-  const int tile = plan.tile_of(in_head), steps = plan.steps(tile);
-  const int first = u - (in_head - static_cast<int>(plan.before(tile)));       // the tile's first unit
-  if (first == u) return;                                // the range begins with the tile
-  const int w0 = ranges.of(first), w1 = ranges.of(first + steps - 1);
-  if (w0 != w - 1) return;
-  const int first_slot = 2 * w0 + (ranges.begin(w0) < first ? 1 : 0);      // the others begin their range
-  const int i0 = tile << a.q_shift, rows = min(rq.n - i0, 1 << a.q_shift) * a.group;
+  const Cut cut = a.cuts[w];
+  // (the tile's first `setup` units are no steps: a range that has none but those leaves nothing)
+  const int first = cut.first + a.setup, w0 = ranges.of(first), w1 = ranges.of(first + cut.steps - 1);
+  if (w0 != w - 1) return;                               // the range begins with the tile, or is not the second of its ranges
+  const int first_slot = 2 * w0 + (ranges.begin(w0) < cut.first ? 1 : 0);      // the others begin their range
+  const int rows = cut.rows;
   const int count = w1 - w0 + 1;
   for (int r = blockIdx.y * kRows + threadIdx.x / kLanes; r < rows; r += gridDim.y * kRows) {
     auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? first_slot : 2 * (w0 + i)) * RT + r; };
@@ -414,7 +464,7 @@ __global__ __launch_bounds__(128) void prompt_merge(PromptParams a) {
     }
 #pragma unroll
     for (int k = kLanes / 2; k > 0; k >>= 1) l += __shfl_xor(l, k, kLanes);
-    const int64_t to = static_cast<int64_t>(rq.row0 + i0 + r / a.group) * kv.num_q_heads + g * a.group + r % a.group;
+    const int64_t to = static_cast<int64_t>(cut.row + r / a.group) * a.kv.num_q_heads + cut.head + r % a.group;
     if (part == 0 && a.lse) a.lse[to] = (l == 0.f ? -INFINITY : m + log2f(l)) * kLn2;
     store_four(a, to * D + 4 * part, x * (l == 0.f ? 0.f : 1.f / l));
   }
@@ -422,8 +472,9 @@ __global__ __launch_bounds__(128) void prompt_merge(PromptParams a) {
 
 // ------------------------------------------------------------------ host --
 struct PromptPlan {
-  int rt, ts, q_shift, ranges;
+  int rt, ts, q_shift, ranges, setup;
   int64_t tiles, units, slots; // (request, head, tile of rows) and units there may be; partial results
+  bool bypass;                 // rows of the cache are read once: they bypass the Infinity Cache
 };
 
 // Wavefronts side by side on the rows: as many groups of 32 as a request may have rows, up to 8; the others of a workgroup of four take other tokens.
@@ -445,9 +496,15 @@ PromptPlan plan_of(const KvView& kv, int total_rows, int max_new, bool f32) {
     p.ts = groups <= 1 ? 128 : 64;
     per_cu = p.rt <= 128 ? 2 : 1;
   }
+  // Beginning and ending a tile (its place, queries, first rows of the cache, results) takes about as long as four steps of 128 or 256 rows, so it counts for
+  // that many in the cutting of the ranges: else ranges of many short tiles, as the first ones of a prompt are, end last.  Counted as none / 2 / 4 / 6 / 8 steps:
+  // 4 prompts of 8 K tokens 2660 / 2593 / 2513 / 2514 / 2513 us, one of 2 K 112 / 80 / 73 / 78 / 79, short ones over fp8 74 / 63 / 62 / 68 / 73.  Tiles of
+  // single tokens: none / 1 / 2 / 4: 64 contexts of 1-8 K 190 / 189 / 191 / 196.
+  p.setup = p.rt >= 128 ? 4 : 1;
   p.q_shift = tile_tokens_shift(p.rt, group);
   p.tiles = tiles_of(p.rt);
-  p.units = p.tiles * ((kv.max_seq_len + p.ts - 1) / p.ts);
+  p.units = p.tiles * ((kv.max_seq_len + p.ts - 1) / p.ts + p.setup);
+  p.bypass = p.rt == 32 && tree_bypasses(static_cast<int64_t>(kv.batch) * kv.num_kv_heads * kv.max_seq_len * 4 * kv.head_dim);
   p.ranges = static_cast<int>(std::min<int64_t>(p.units, static_cast<int64_t>(per_cu) * num_cus()));
   p.slots = 2 * static_cast<int64_t>(p.ranges);
   return p;
@@ -458,7 +515,7 @@ struct PromptWs {
 };
 PromptWs carve(const KvView& kv, int64_t slots, int rt) {
   PromptWs w;
-  size_t at = align_up((static_cast<size_t>(kv.batch) + 1) * 4, 256);
+  size_t at = align_up(256 + static_cast<size_t>(slots / 2) * sizeof(Cut), 256);
   w.ml = at;
   at = align_up(at + static_cast<size_t>(slots) * rt * 8, 256);
   w.o = at;
@@ -466,12 +523,12 @@ PromptWs carve(const KvView& kv, int64_t slots, int rt) {
   return w;
 }
 
-template <typename C>
+template <typename C, typename N>
 hipError_t launch_as(const PromptParams& p, const PromptPlan& plan, hipStream_t s) {
-  static_assert(C::kLds + 12 * C::TS + 64 * C::kWaves * 4 + C::RT / 4 <= 160 * 1024, "");
+  static_assert((C::kLds > N::kLds ? C::kLds : N::kLds) + 12 * (C::TS > N::TS ? C::TS : N::TS) + 64 * C::kWaves * 4 + 64 <= 160 * 1024, "");
   {
     KernelTimer timer("prompt_pass", s);
-    hipLaunchKernelGGL((prompt_pass<C>), dim3(p.ranges), dim3(C::kThreads), 0, s, p);
+    hipLaunchKernelGGL((prompt_pass<C, N>), dim3(p.ranges), dim3(C::kThreads), 0, s, p);
   }
   if (p.ranges > 1) {
     KernelTimer timer("prompt_merge", s);
@@ -480,26 +537,31 @@ hipError_t launch_as(const PromptParams& p, const PromptPlan& plan, hipStream_t 
     const int64_t busy = std::min<int64_t>(p.ranges - 1, plan.tiles);
     const int room = static_cast<int>(std::max<int64_t>(1, 16 * num_cus() / busy));
     const dim3 grid(p.ranges - 1, std::min(room, (rows + kRows - 1) / kRows));
-    if (p.ranges > 4 * plan.tiles) hipLaunchKernelGGL((prompt_merge<C::D, C::TS, C::RT, 16>), grid, dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((prompt_merge<C::D, C::TS, C::RT, 4>), grid, dim3(kThreads), 0, s, p);
+    if (p.ranges > 4 * plan.tiles) hipLaunchKernelGGL((prompt_merge<C::D, C::RT, 16>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((prompt_merge<C::D, C::RT, 4>), grid, dim3(kThreads), 0, s, p);
   }
   return hipGetLastError();
 }
 
 template <int D, int KV>
 hipError_t launch_bf16(const PromptParams& p, const PromptPlan& plan, hipStream_t s) {
+  using N4 = Cfg<D, KV, false, 1, 4, 1, false>;
+  using N2 = Cfg<D, KV, false, 2, 2, 1, false>;
   switch (plan.rt) {
-    case 32: return launch_as<Cfg<D, KV, false, 1, 4, 1, false>>(p, plan, s);
-    case 64: return launch_as<Cfg<D, KV, false, 2, 2, 1, false>>(p, plan, s);
-    case 128: return launch_as<Cfg<D, KV, false, 4, 1, 2, false>>(p, plan, s);
-    default: return launch_as<Cfg<D, KV, false, 8, 1, 2, false>>(p, plan, s);
+    case 32:
+      if (plan.bypass) return launch_as<Cfg<D, KV, false, 1, 4, 1, true>, Cfg<D, KV, false, 1, 4, 1, true>>(p, plan, s);
+      return launch_as<N4, N4>(p, plan, s);
+    case 64: return launch_as<N2, N2>(p, plan, s);
+    case 128: return launch_as<Cfg<D, KV, false, 4, 1, 2, false>, N2>(p, plan, s);
+    default: return launch_as<Cfg<D, KV, false, 8, 1, 2, false>, Cfg<D, KV, false, 2, 4, 1, false>>(p, plan, s);
   }
 }
 template <int D, int KV>
 hipError_t launch_f32(const PromptParams& p, const PromptPlan& plan, hipStream_t s) {
-  if (plan.rt == 32) return launch_as<Cfg<D, KV, true, 1, 4, 1, false>>(p, plan, s);
-  if (plan.rt == 64) return launch_as<Cfg<D, KV, true, 2, 2, 1, false>>(p, plan, s);
-  return launch_as<Cfg<D, KV, true, 4, 1, 2, false>>(p, plan, s);
+  using N4 = Cfg<D, KV, true, 1, 4, 1, false>;
+  if (plan.rt == 32) return launch_as<N4, N4>(p, plan, s);
+  if (plan.rt == 64) return launch_as<Cfg<D, KV, true, 2, 2, 1, false>, Cfg<D, KV, true, 2, 2, 1, false>>(p, plan, s);
+  return launch_as<Cfg<D, KV, true, 4, 1, 2, false>, Cfg<D, KV, true, 4, 1, 2, false>>(p, plan, s);
 }
 
 }  // namespace
@@ -532,9 +594,12 @@ hipError_t launch_prompt(const PromptArgs& t, hipStream_t s) {
   p.group = kv.num_q_heads / kv.num_kv_heads;
   p.q_dtype = t.q_dtype;
   p.q_shift = plan.q_shift;
+  p.setup = plan.setup;
+  p.part_rows = plan.rt;
   p.aligned = rows_aligned(kv, t.kv_dtype);
   p.dense = dense;
-  p.prefix = reinterpret_cast<int32_t*>(ws);
+  p.total = reinterpret_cast<int32_t*>(ws);
+  p.cuts = reinterpret_cast<Cut*>(ws + 256);
   p.part_ml = reinterpret_cast<float*>(ws + w.ml);
   p.part_o = reinterpret_cast<float*>(ws + w.o);
   p.ranges = plan.ranges;

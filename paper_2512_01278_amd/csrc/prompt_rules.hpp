@@ -2,7 +2,7 @@
 //
 // A request's n new tokens, the last of its `len`, are taken 2^q_shift to a tile; the cache is read 2^t_shift tokens at a step.  Tile r sees no
 // more than the tokens up to its last row's, so it has min(cap, ceil((first + (r + 1) Q) / T)) steps, first = len - n, cap = ceil(len / T); a unit is one
-// step of one tile of one KV head.  Q and T are powers of two, so the units before a tile have a closed form, and a unit's tile is found by halving.
+// step of one tile of one KV head.  Q and T are powers of two, so the units before a tile have a closed form, and a unit's tile is near a root.
 #pragma once
 
 #include <cstdint>
@@ -15,47 +15,61 @@ namespace pillar {
 #define PILLAR_RULE inline
 #endif
 
+// Everything below is 32-bit arithmetic without sign: counts of units are below 2^31, and where a term is larger on the way, only differences of such terms are
+// taken, which come out right modulo 2^32.  (In 64 bits the search below took the kernels 2 us, and the one that joins partials, where every
+// wavefront searches, 17 of its 25.)
 struct PromptSteps {
   int q_shift, t_shift;
-  int from;                    // tokens before, rounded up to steps, and a tile: the numerator of the first tile's steps
+  uint32_t from;               // tokens before, rounded up to steps, and a tile: the numerator of the first tile's steps
   int cap;
   int tiles;                   // 0: nothing to do (no new token, or none in the cache)
+  int setup;                   // units that a tile has beside its steps, ahead of them: what it costs to begin and end one
 
-  PILLAR_RULE PromptSteps(int len, int n, int q_shift_, int t_shift_) : q_shift(q_shift_), t_shift(t_shift_) {
-    const int first = len > n ? len - n : 0;             // (rows whose number would be negative see nothing; their tiles have a few steps all the same)
-    from = first + (1 << t_shift) - 1 + (1 << q_shift);
-    cap = (len + (1 << t_shift) - 1) >> t_shift;
-    tiles = len > 0 && n > 0 ? (n + (1 << q_shift) - 1) >> q_shift : 0;
+  PILLAR_RULE PromptSteps(int len, int n, int q_shift_, int t_shift_, int setup_) : q_shift(q_shift_), t_shift(t_shift_), setup(setup_) {
+    const uint32_t first = len > n ? len - n : 0;        // (rows whose number would be negative see nothing; their tiles have a few steps all the same)
+    from = first + (1u << t_shift) - 1 + (1u << q_shift);
+    cap = static_cast<int>((static_cast<uint32_t>(len) + (1u << t_shift) - 1) >> t_shift);
+    tiles = len > 0 && n > 0 ? static_cast<int>((static_cast<uint32_t>(n) + (1u << q_shift) - 1) >> q_shift) : 0;
   }
   PILLAR_RULE int steps(int r) const {
-    const int64_t s = (from + (static_cast<int64_t>(r) << q_shift)) >> t_shift;
-    return s < cap ? static_cast<int>(s) : cap;
+    const int s = static_cast<int>((from + (static_cast<uint32_t>(r) << q_shift)) >> t_shift);
+    return s < cap ? s : cap;
   }
-  // sum over i < n of i >> d
-  static PILLAR_RULE int64_t sum_of_shifted(int64_t n, int d) {
-    const int64_t k = n >> d;
-    return ((k * (k - 1) / 2) << d) + (n - (k << d)) * k;
+  // 0 + 1 + ... + k - 1, modulo 2^32
+  static PILLAR_RULE uint32_t up_to(uint32_t k) { return (k & 1) ? k * ((k - 1) >> 1) : (k >> 1) * (k - 1); }
+  // sum over i < n of i >> d, modulo 2^32
+  static PILLAR_RULE uint32_t sum_of_shifted(uint32_t n, int d) {
+    const uint32_t k = n >> d;
+    return (up_to(k) << d) + (n - (k << d)) * k;
   }
   // units of the tiles before r, r <= tiles
-  PILLAR_RULE int64_t before(int r) const {
+  PILLAR_RULE int before(int r) const {
     const int d = q_shift - t_shift;
     if (d >= 0) {                                        // steps(r) = a + (r << d) as long as that is below cap
-      const int64_t a = from >> t_shift, room = cap > a ? (cap - a + (1 << d) - 1) >> d : 0, k = room < r ? room : r;
-      return k * a + ((k * (k - 1) / 2) << d) + (r - k) * cap;
+      const int a = static_cast<int>(from >> t_shift), room = cap > a ? (cap - a + (1 << d) - 1) >> d : 0, k = room < r ? room : r;
+      return static_cast<int>(static_cast<uint32_t>(k) * a + (up_to(k) << d) + static_cast<uint32_t>(r - k) * cap + static_cast<uint32_t>(r) * setup);
     }
-    const int64_t a = from >> q_shift, room = (static_cast<int64_t>(cap) << -d) - a, k = room < 0 ? 0 : room < r ? room : r;
-    return sum_of_shifted(a + k, -d) - sum_of_shifted(a, -d) + (r - k) * cap;
+    const uint32_t a = from >> q_shift;
+    const int room = static_cast<int>((static_cast<uint32_t>(cap) << -d) - a), k = room < 0 ? 0 : room < r ? room : r;
+    return static_cast<int>(sum_of_shifted(a + k, -d) - sum_of_shifted(a, -d) + static_cast<uint32_t>(r - k) * cap + static_cast<uint32_t>(r) * setup);
   }
-  PILLAR_RULE int units() const { return tiles > 0 ? static_cast<int>(before(tiles)) : 0; }
+  PILLAR_RULE int units() const { return tiles > 0 ? before(tiles) : 0; }
   // the tile that has unit u, 0 <= u < units()
   PILLAR_RULE int tile_of(int u) const {
-    int lo = 0, hi = tiles;                              // before(lo) <= u < before(hi)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (before(mid) <= u) lo = mid;
-      else hi = mid;
-    }
-    return lo;
+    // steps grow by Q / T from tile to tile, so the units before tile r are about (s - 1/2 step) r + Q / T r^2 / 2: its root, and then the few tiles it is off by
+    const float grow = static_cast<float>(1 << q_shift) / static_cast<float>(1 << t_shift), s = static_cast<float>(steps(0) + setup) - 0.5f * grow;
+    int r = static_cast<int>(2.f * static_cast<float>(u) / (s + sqrt_of(s * s + 2.f * grow * static_cast<float>(u))));
+    r = r < 0 ? 0 : r >= tiles ? tiles - 1 : r;
+    while (r > 0 && before(r) > u) --r;
+    while (r + 1 < tiles && before(r + 1) <= u) ++r;
+    return r;
+  }
+  static PILLAR_RULE float sqrt_of(float x) {
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_sqrtf(x);
+#else
+    return __builtin_sqrtf(x);
+#endif
   }
 };
 

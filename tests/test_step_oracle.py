@@ -121,9 +121,9 @@ MAIN = r"""
 #include <cstdlib>
 #include "prompt_rules.hpp"
 int main(int argc, char** v) {
-  const pillar::PromptSteps p(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]));
+  const pillar::PromptSteps p(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[6]));
   printf("%d %d\n", p.tiles, p.units());
-  for (int r = 0; r < p.tiles; ++r) printf("%d %lld\n", p.steps(r), static_cast<long long>(p.before(r)));
+  for (int r = 0; r < p.tiles; ++r) printf("%d %d\n", p.steps(r), p.before(r));
   const int units = p.units();
   for (int u = 0; u < units; u += units > 5000 ? 37 : 1) printf("%d %d\n", u, p.tile_of(u));
   printf("%d %d\n", pillar::tile_tokens_shift(256, atoi(v[5])), pillar::tile_tokens_shift(32, atoi(v[5])));
@@ -140,11 +140,12 @@ def rule(tmp_path_factory):
                           subprocess.run([str(d / "rule"), *map(str, args)], check=True, capture_output=True, text=True).stdout.splitlines()]
 
 
+@pytest.mark.parametrize("setup", [0, 2])
 @pytest.mark.parametrize("q_shift,t_shift", [(0, 6), (1, 7), (4, 6), (5, 6), (6, 6), (7, 6), (8, 6), (3, 7)])
 @pytest.mark.parametrize("length,n", [(1, 1), (64, 64), (65, 65), (1000, 1000), (1000, 1), (4097, 513), (130, 129), (5, 9), (200, 1000), (0, 3), (7, 0), (30000, 700)])
-def test_units_of_a_prompt(rule, length, n, q_shift, t_shift):
+def test_units_of_a_prompt(rule, length, n, q_shift, t_shift, setup):
     """Against the definition: every tile's steps reach its last row's token, never past the cache, and each unit has its tile."""
-    lines = rule(length, n, q_shift, t_shift, 5)
+    lines = rule(length, n, q_shift, t_shift, 5, setup)
     Q, T = 1 << q_shift, 1 << t_shift
     tiles = -(-n // Q) if length > 0 else 0
     steps = [s for s, _ in lines[1:1 + tiles]]
@@ -152,6 +153,7 @@ def test_units_of_a_prompt(rule, length, n, q_shift, t_shift):
     for r, s in enumerate(steps):
         need = -(-max(0, min(length, first + (r + 1) * Q)) // T)
         assert s >= need and s <= -(-length // T) and (s == need or first < 0), (r, s, need)
+    steps = [s + setup for s in steps]
     assert lines[0] == (tiles, sum(steps))
     assert [b for _, b in lines[1:1 + tiles]] == [sum(steps[:r]) for r in range(tiles)]
     ends = np.cumsum(steps)
@@ -161,7 +163,7 @@ def test_units_of_a_prompt(rule, length, n, q_shift, t_shift):
 
 
 def test_units_of_a_very_long_context_do_not_overflow(rule):
-    lines = rule(16_000_000, 40, 4, 6, 16)
+    lines = rule(16_000_000, 40, 4, 6, 16, 0)
     assert lines[0][0] == 3 and abs(lines[0][1] - 3 * 250_000) <= 3
     assert lines[-1] == (4, 1)
 
