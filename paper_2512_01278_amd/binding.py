@@ -463,26 +463,27 @@ def _current(t: torch.Tensor, what: str) -> int:
     return dev
 
 
-def _head_rows(t: Optional[torch.Tensor], dtype: torch.dtype, rows: Optional[int], heads: Optional[int], D: Optional[int], dev: int, what: str) -> tuple:
+def _head_rows(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, dev: int, what: str) -> tuple:
     """Address and row stride of [rows][heads][D] whose heads are dense; the rows may lie apart."""
     if t is None:
         return None, 0
-    shape, strides = t.shape, t.stride()
-    fits = len(shape) == 3 and (rows is None or shape[0] == rows) and (heads is None or shape[1] == heads) and (D is None or shape[2] == D)
-    # (the stride of an axis of one says nothing)
-    dense = fits and (strides[2] == 1 or shape[2] == 1) and (strides[1] == shape[2] or shape[1] == 1)
-    if t.dtype is not dtype or t.get_device() != dev or not dense:
-        _refuse(t, what, f"{dtype} tensor [{rows or 'tokens'}, {heads or 'heads'}, {D or 'head_dim'}], dense but for its rows,", dev)
-    return t.data_ptr(), strides[0] if shape[0] > 1 else max(strides[0], shape[1] * shape[2])
+    rows, heads, D = shape
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse(t, what, f"{dtype} tensor of shape {tuple(shape)}, dense but for its rows,", dev)
+    apart, of_head, of_dim = t.stride()
+    if of_dim != 1 or of_head != D:
+        if (of_dim != 1 and D != 1) or (of_head != D and heads != 1):       # (the stride of an axis of one says nothing)
+            _refuse(t, what, f"{dtype} tensor of shape {tuple(shape)}, dense but for its rows,", dev)
+    return t.data_ptr(), apart if rows > 1 else heads * D
 
 
 def pillar_rotate(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: torch.Tensor, stream=None) -> None:
     dev = _current(x, "x")
     if x.dtype not in _DTYPE_OF or x.dim() != 3:
         _refuse(x, "x", "fp32 or bf16 tensor [tokens, heads, head_dim]", dev)
-    T, H, D = x.shape
-    x_at, x_stride = _head_rows(x, x.dtype, T, H, D, dev, "x")
-    out_at, out_stride = _head_rows(out, x.dtype, T, H, D, dev, "out")
+    shape = T, H, D = x.shape
+    x_at, x_stride = _head_rows(x, x.dtype, shape, dev, "x")
+    out_at, out_stride = _head_rows(out, x.dtype, shape, dev, "out")
     r = rope.c_struct(dev)
     rc = load().pillar_rotate(x_at, x_stride, T, H, D, _DTYPE_OF[x.dtype], _per_request(positions, T, dev, "positions"), C.byref(r), out_at, out_stride,
                               _stream(stream))
@@ -493,14 +494,15 @@ def pillar_append_rotated(kv: KvCache, rope: Optional[Rope], k_new: torch.Tensor
                           starts: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
                           q_out: Optional[torch.Tensor] = None, stream=None) -> None:
     s, dev = kv.c_struct(), _device(kv)
-    T, qt = k_new.shape[0], _Q_TORCH[kv.q_dtype]
-    k_at, k_stride = _head_rows(k_new, qt, T, s.num_kv_heads, s.head_dim, dev, "k_new")
-    v_at, v_stride = _head_rows(v_new, qt, T, s.num_kv_heads, s.head_dim, dev, "v_new")
-    q_at, q_stride = _head_rows(q, qt, T, s.num_q_heads, s.head_dim, dev, "q")
+    T, D, qt = k_new.shape[0], s.head_dim, _Q_TORCH[kv.q_dtype]
+    rows, q_rows = (T, s.num_kv_heads, D), (T, s.num_q_heads, D)
+    k_at, k_stride = _head_rows(k_new, qt, rows, dev, "k_new")
+    v_at, v_stride = _head_rows(v_new, qt, rows, dev, "v_new")
+    q_at, q_stride = _head_rows(q, qt, q_rows, dev, "q")
     r = None if rope is None else C.byref(rope.c_struct(dev))
     rc = load().pillar_append_rotated(C.byref(s), r, _per_request(starts, s.batch + 1, dev, "starts"), T, max_new,
-                                      _per_request(positions, T, dev, "positions"), q_at, q_stride,
-                                      _tensor(q_out, qt, (T, s.num_q_heads, s.head_dim), dev, "q_out"), k_at, k_stride, v_at, v_stride, _stream(stream))
+                                      _per_request(positions, T, dev, "positions"), q_at, q_stride, _tensor(q_out, qt, q_rows, dev, "q_out"),
+                                      k_at, k_stride, v_at, v_stride, _stream(stream))
     _check(rc, "pillar_append_rotated")
 
 

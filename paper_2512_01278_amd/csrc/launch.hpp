@@ -225,6 +225,7 @@ struct LogprobArgs {
 };
 
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
+bool append_fits_a_grid(const AppendArgs& a);
 hipError_t launch_append_rotated(const AppendArgs& a, hipStream_t s);
 bool prompt_counts(const KvView& kv, int total_rows, int max_new);           // the units of work can be counted in 32 bits
 size_t prompt_workspace(const KvView& kv, int total_rows, int max_new);

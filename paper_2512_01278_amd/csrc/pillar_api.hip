@@ -714,6 +714,7 @@ int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, cons
   a.v_stride = v_stride;
   a.q_dtype = kv->q_dtype;
   a.kv_dtype = kv->kv_dtype;
+  if (!append_fits_a_grid(a)) return PILLAR_EUNSUPPORTED;
   return launch_append_rotated(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PILLAR_OK : PILLAR_EHIP;
 }
 

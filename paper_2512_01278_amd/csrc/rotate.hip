@@ -328,6 +328,19 @@ __global__ __launch_bounds__(kThreads) void append_pages(AppendArgs a, int pages
   }
 }
 
+// Pages that may receive rows: n rows lie in (n - 2) / page_size + 2 pages at most; all of them in no more than total_rows / page_size and two for each request.
+struct Pages {
+  int64_t each, all, workgroups;
+};
+Pages pages_of(const AppendArgs& a) {
+  Pages p;
+  p.each = (std::min<int64_t>(a.max_new, a.kv.max_seq_len) + 2 * a.kv.page_size - 2) / a.kv.page_size;
+  p.all = p.each * a.kv.batch;
+  if (a.starts) p.all = std::min<int64_t>(p.all, a.total_rows / a.kv.page_size + 2 * static_cast<int64_t>(a.kv.batch));
+  p.workgroups = p.all * a.kv.num_kv_heads + (a.q ? a.total_rows : 0);
+  return p;
+}
+
 template <int DT, int V>
 hipError_t rotate(const RotateArgs& a, hipStream_t s) {
   KernelTimer timer("rotate_rows", s);
@@ -339,13 +352,8 @@ template <int DT, int V>
 hipError_t append(const AppendArgs& a, hipStream_t s) {
   if (a.kv_dtype == PILLAR_FP8_E4M3) {
     KernelTimer timer("append_pages", s);
-    // n rows lie in (n - 2) / page_size + 2 pages at most; all of them in no more than total_rows / page_size and two for each request
-    const int64_t pages_each = (std::min<int64_t>(a.max_new, a.kv.max_seq_len) + 2 * a.kv.page_size - 2) / a.kv.page_size;
-    int64_t pages = pages_each * a.kv.batch;
-    if (a.starts) pages = std::min<int64_t>(pages, a.total_rows / a.kv.page_size + 2 * static_cast<int64_t>(a.kv.batch));
-    const int64_t workgroups = pages * a.kv.num_kv_heads + (a.q ? a.total_rows : 0);
-    if (workgroups > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((append_pages<DT, V>), dim3(static_cast<unsigned>(workgroups)), dim3(kThreads), 0, s, a, static_cast<int>(pages_each), static_cast<int>(pages));
+    const Pages p = pages_of(a);
+    hipLaunchKernelGGL((append_pages<DT, V>), dim3(static_cast<unsigned>(p.workgroups)), dim3(kThreads), 0, s, a, static_cast<int>(p.each), static_cast<int>(p.all));
     return hipGetLastError();
   }
   KernelTimer timer("append_rows", s);
@@ -364,6 +372,8 @@ hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) {
   if (a.dtype == PILLAR_F32) return pieces ? rotate<PILLAR_F32, 4>(a, s) : rotate<PILLAR_F32, 1>(a, s);
   return pieces ? rotate<PILLAR_BF16, 8>(a, s) : rotate<PILLAR_BF16, 1>(a, s);
 }
+
+bool append_fits_a_grid(const AppendArgs& a) { return a.kv_dtype != PILLAR_FP8_E4M3 || pages_of(a).workgroups <= INT32_MAX; }
 
 hipError_t launch_append_rotated(const AppendArgs& a, hipStream_t s) {
   const bool pieces = rope_in_pieces(a.rope, a.kv.head_dim, a.q_dtype == PILLAR_F32 ? 4 : 8);
