@@ -266,7 +266,8 @@ struct Row {
   }
   __device__ __forceinline__ void put_sums() const {
     if (a.lse) a.lse[r] = nan ? NAN : empty ? -INFINITY : endless ? INFINITY : __builtin_fmaf(a.scale, sums.m, log_s);
-    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty ? 0.f : log_s - kLn2 * (sums.a / sums.s);
+    const float h = log_s - kLn2 * (sums.a / sums.s);    // (a little below 0 by rounding where one token has it all)
+    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty || h < 0.f ? 0.f : h;
   }
   // (one wavefront) Fewer numbers above -inf than wanted: the first of -inf, then the first that are none at all.
   __device__ __forceinline__ void put_list(List list) const {

@@ -14,8 +14,6 @@ namespace pillar {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // cosine and sine of position * frequency, times amplitude
@@ -36,21 +34,21 @@ __device__ __forceinline__ float2 turned(int position, double frequency, float a
   return make_float2(cosine * amplitude, sine * amplitude);
 }
 
-// V elements as fp32
+// V elements as fp32, V of 1, 2, 4, 8 (bf16) in one load
 template <int DT, int V>
 __device__ __forceinline__ void load_elems(const void* p, int64_t at, float (&x)[V]) {
   if constexpr (V == 1) {
     x[0] = Storage<DT>::load(p, at);
   } else if constexpr (DT == PILLAR_F32) {
-    static_assert(V == 4, "");
-    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p) + at);
+    typedef float Vec __attribute__((ext_vector_type(V)));
+    const Vec v = *reinterpret_cast<const Vec*>(static_cast<const float*>(p) + at);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = v[j];
+    for (int j = 0; j < V; ++j) x[j] = v[j];
   } else {
-    static_assert(V == 8, "");
-    const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at);
+    typedef uint16_t Vec __attribute__((ext_vector_type(V)));
+    const Vec v = *reinterpret_cast<const Vec*>(static_cast<const uint16_t*>(p) + at);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float((j & 1) ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
+    for (int j = 0; j < V; ++j) x[j] = bf16_to_f32(v[j]);
   }
 }
 
@@ -60,18 +58,21 @@ __device__ __forceinline__ void store_elems(void* p, int64_t at, const float (&x
   if constexpr (V == 1) {
     Storage<DT>::store(p, at, x[0]);
   } else if constexpr (DT == PILLAR_F32) {
+    constexpr int W = V < 4 ? V : 4;
+    typedef float Vec __attribute__((ext_vector_type(W)));
 #pragma unroll
-    for (int j = 0; j < V; j += 4) *reinterpret_cast<f32x4_t*>(static_cast<float*>(p) + at + j) = f32x4_t{x[j], x[j + 1], x[j + 2], x[j + 3]};
-  } else if constexpr (V == 4) {
-    bf16x4_t y;
+    for (int j = 0; j < V; j += W) {
+      Vec y;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = static_cast<__bf16>(x[j]);
-    *reinterpret_cast<bf16x4_t*>(static_cast<uint16_t*>(p) + at) = y;
+      for (int k = 0; k < W; ++k) y[k] = x[j + k];
+      *reinterpret_cast<Vec*>(static_cast<float*>(p) + at + j) = y;
+    }
   } else {
-    bf16x8_t y;
+    typedef __bf16 Vec __attribute__((ext_vector_type(V)));
+    Vec y;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = static_cast<__bf16>(x[j]);
-    *reinterpret_cast<bf16x8_t*>(static_cast<uint16_t*>(p) + at) = y;
+    for (int j = 0; j < V; ++j) y[j] = static_cast<__bf16>(x[j]);
+    *reinterpret_cast<Vec*>(static_cast<uint16_t*>(p) + at) = y;
   }
 }
 
@@ -97,10 +98,27 @@ __host__ __device__ __forceinline__ int pieces_of_head(const RopeView& rope, int
   const int turning = V > 1 && rope.interleaved ? 2 * rope.half / V : rope.half / V;
   return turning + (D - 2 * rope.half) / V;
 }
-// whether pieces of V > 1 elements will do
+// whether pieces of V elements will do
 inline bool rope_in_pieces(const RopeView& rope, int D, int V) {
   return D % V == 0 && (rope.interleaved ? 2 * rope.half : rope.half) % V == 0;
 }
+
+// Head and piece of a thread, turn by turn, without a division in each.
+struct HeadPiece {
+  int h, c;
+  int pieces, heads_on, pieces_on;
+  __device__ __forceinline__ HeadPiece(int pieces_, int threads) : pieces(pieces_) {
+    h = static_cast<int>(threadIdx.x) / pieces;
+    c = static_cast<int>(threadIdx.x) - h * pieces;
+    heads_on = threads / pieces;
+    pieces_on = threads - heads_on * pieces;
+  }
+  __device__ __forceinline__ void next() {
+    h += heads_on;
+    c += pieces_on;
+    if (c >= pieces) { c -= pieces; ++h; }
+  }
+};
 
 // turns a piece (in the same operations whatever V is: the same bits); angle(i): cosine and sine of its i-th pair
 template <int V, typename Angle>

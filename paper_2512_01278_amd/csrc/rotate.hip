@@ -8,6 +8,7 @@
 // with keys and values into their pages (638 MB) in 132 us, both at the rate of a large copy (4.8 TB/s).  Turns are worked out once per row, into LDS, for all its heads.
 // Where there is little, by the launch: one token 4.7 us, of which the chain starts, lengths, page id, rows is the most.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "page_scale.hpp"
@@ -57,10 +58,9 @@ __global__ __launch_bounds__(kThreads) void rotate_rows(RotateArgs a) {
   __syncthreads();
   const int pieces = pieces_of_head<V>(a.rope, a.head_dim);
   const int64_t from = t * a.x_stride, to = t * a.out_stride;
-  for (int e = tid; e < a.heads * pieces; e += kThreads) {
-    const int h = e / pieces;
-    const Piece p = piece_of<V>(a.rope, e - h * pieces);
-    const int64_t head = static_cast<int64_t>(h) * a.head_dim;
+  for (HeadPiece at(pieces, kThreads); at.h < a.heads; at.next()) {
+    const Piece p = piece_of<V>(a.rope, at.c);
+    const int64_t head = static_cast<int64_t>(at.h) * a.head_dim;
     float x[V], y[V] = {};
     load_elems<DT, V>(a.x, from + head + p.lo, x);
     if (p.hi >= 0) load_elems<DT, V>(a.x, from + head + p.hi, y);
@@ -94,10 +94,9 @@ __device__ __forceinline__ bool begin_row(const AppendArgs& a, int t, Row& row, 
 template <int DT, int V>
 __device__ __forceinline__ void turn_queries(const AppendArgs& a, int t, const float2* s_turn) {
   const int D = a.kv.head_dim, pieces = pieces_of_head<V>(a.rope, D);
-  for (int e = threadIdx.x; e < a.kv.num_q_heads * pieces; e += kThreads) {
-    const int h = e / pieces;
-    const int64_t to = (static_cast<int64_t>(t) * a.kv.num_q_heads + h) * D;
-    turn_and_store<DT, V>(a.rope, a.q, t * a.q_stride + static_cast<int64_t>(h) * D, e - h * pieces, s_turn,
+  for (HeadPiece at(pieces, kThreads); at.h < a.kv.num_q_heads; at.next()) {
+    const int64_t to = (static_cast<int64_t>(t) * a.kv.num_q_heads + at.h) * D;
+    turn_and_store<DT, V>(a.rope, a.q, t * a.q_stride + static_cast<int64_t>(at.h) * D, at.c, s_turn,
                           [&](int dim, const float (&x)[V]) { store_elems<DT, V>(a.q_out, to + dim, x); });
   }
 }
@@ -117,17 +116,16 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
   if (a.q) turn_queries<DT, V>(a, t, s_turn);
   if (token < 0) return;
   int page;
-  for (int e = tid; e < a.kv.num_kv_heads * pieces; e += kThreads) {
-    const int g = e / pieces;
-    const int64_t to = row_offset(a.kv, row.b, g, token, &page);
-    turn_and_store<DT, V>(a.rope, a.k_new, t * a.k_stride + static_cast<int64_t>(g) * D, e - g * pieces, s_turn,
+  for (HeadPiece at(pieces, kThreads); at.h < a.kv.num_kv_heads; at.next()) {
+    const int64_t to = row_offset(a.kv, row.b, at.h, token, &page);
+    turn_and_store<DT, V>(a.rope, a.k_new, t * a.k_stride + static_cast<int64_t>(at.h) * D, at.c, s_turn,
                           [&](int dim, const float (&x)[V]) { store_elems<KV, V>(const_cast<void*>(a.kv.k_pool), to + dim, x); });
   }
-  for (int e = tid; e < a.kv.num_kv_heads * (D / V); e += kThreads) {
-    const int g = e / (D / V), dim = (e - g * (D / V)) * V;
-    float x[V];
-    load_elems<DT, V>(a.v_new, t * a.v_stride + static_cast<int64_t>(g) * D + dim, x);
-    store_elems<KV, V>(const_cast<void*>(a.kv.v_pool), row_offset(a.kv, row.b, g, token, &page) + dim, x);
+  constexpr int W = DT == PILLAR_F32 ? 4 : 8;            // (values are not turned: in 16 bytes whatever V is)
+  for (HeadPiece at(D / W, kThreads); at.h < a.kv.num_kv_heads; at.next()) {
+    float x[W];
+    load_elems<DT, W>(a.v_new, t * a.v_stride + static_cast<int64_t>(at.h) * D + at.c * W, x);
+    store_elems<KV, W>(const_cast<void*>(a.kv.v_pool), row_offset(a.kv, row.b, at.h, token, &page) + at.c * W, x);
   }
 }
 
@@ -176,8 +174,9 @@ struct PageOf {
 // V codes, one behind the other
 template <int V>
 __device__ __forceinline__ void store_codes(uint8_t* to, const float (&x)[V], float inv) {
-  if constexpr (V == 1) {
-    *to = code_of(x[0] * inv);
+  if constexpr (V < 4) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) to[j] = code_of(x[j] * inv);
   } else {
     uint32_t w[V / 4];
 #pragma unroll
@@ -362,23 +361,39 @@ hipError_t append(const AppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool multiple_of_16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// calls f with the largest pieces that will do: 16 bytes, half of that, and so on
+template <int DT, typename Will, typename F>
+hipError_t by_piece(Will will, F f) {
+  if constexpr (DT == PILLAR_BF16) {
+    if (will(8)) return f(std::integral_constant<int, 8>());
+  }
+  if (will(4)) return f(std::integral_constant<int, 4>());
+  if (will(2)) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
+}
+
+template <int DT>
+hipError_t rotate_as(const RotateArgs& a, hipStream_t s) {
+  const int esz = DT == PILLAR_F32 ? 4 : 2;
+  auto will = [&](int V) {
+    return rope_in_pieces(a.rope, a.head_dim, V) && ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.out)) % (V * esz)) == 0 &&
+           a.x_stride % V == 0 && a.out_stride % V == 0;
+  };
+  return by_piece<DT>(will, [&](auto V) { return rotate<DT, V.value>(a, s); });
+}
+template <int DT>
+hipError_t append_as(const AppendArgs& a, hipStream_t s) {
+  return by_piece<DT>([&](int V) { return rope_in_pieces(a.rope, a.kv.head_dim, V); }, [&](auto V) { return append<DT, V.value>(a, s); });
+}
 
 }  // namespace
 
-hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) {
-  const int per = a.dtype == PILLAR_F32 ? 4 : 8;
-  const bool pieces = rope_in_pieces(a.rope, a.head_dim, per) && multiple_of_16(a.x) && multiple_of_16(a.out) && a.x_stride % per == 0 && a.out_stride % per == 0;
-  if (a.dtype == PILLAR_F32) return pieces ? rotate<PILLAR_F32, 4>(a, s) : rotate<PILLAR_F32, 1>(a, s);
-  return pieces ? rotate<PILLAR_BF16, 8>(a, s) : rotate<PILLAR_BF16, 1>(a, s);
-}
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) { return a.dtype == PILLAR_F32 ? rotate_as<PILLAR_F32>(a, s) : rotate_as<PILLAR_BF16>(a, s); }
 
 bool append_fits_a_grid(const AppendArgs& a) { return a.kv_dtype != PILLAR_FP8_E4M3 || pages_of(a).workgroups <= INT32_MAX; }
 
 hipError_t launch_append_rotated(const AppendArgs& a, hipStream_t s) {
-  const bool pieces = rope_in_pieces(a.rope, a.kv.head_dim, a.q_dtype == PILLAR_F32 ? 4 : 8);
-  if (a.q_dtype == PILLAR_F32) return pieces ? append<PILLAR_F32, 4>(a, s) : append<PILLAR_F32, 1>(a, s);
-  return pieces ? append<PILLAR_BF16, 8>(a, s) : append<PILLAR_BF16, 1>(a, s);
+  return a.q_dtype == PILLAR_F32 ? append_as<PILLAR_F32>(a, s) : append_as<PILLAR_BF16>(a, s);
 }
 
 }  // namespace pillar

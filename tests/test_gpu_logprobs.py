@@ -201,3 +201,31 @@ def test_captured_replayed_and_two_at_once():
         torch.cuda.synchronize()
         for c, f in zip(calls, first):
             assert all(torch.equal(t, was) for t, was in zip(outputs(c), f)), turn
+
+
+@pytest.mark.parametrize("dtype,per", [("f32", 4), ("bf16", 8)])
+@pytest.mark.parametrize("top", [1, 3, 9, 64])
+def test_ties_at_the_ends_of_unaligned_rows(dtype, per, top):
+    """A row's first and last logits, up to the next 16 bytes, are read apart from the others: equal ones go by number all the same."""
+    V = 1500 + 3
+    for offset in range(per):
+        x = np.full((4, V), -1.0)
+        x[0] = 0.0
+        x[1, :per], x[1, 700:720], x[1, -per:] = 2.0, 2.0, 2.0
+        x[2, -2:], x[2, 5] = 3.0, 3.0
+        x[3, 0], x[3, 1], x[3, V - 1], x[3, 900] = 1.0, 4.0, 4.0, 4.0
+        Call(x, dtype, ids(4, V, 1), top, offset=offset).run().check()
+
+
+def test_entropy_is_not_negative():
+    x = np.zeros((6, 3000))
+    for r in range(6):
+        x[r, 100 * r] = 10.0 + 7 * r
+    assert (Call(x, "f32", None, 0, 3.0).run().check().entropy >= 0).all()
+
+
+def test_no_rows():
+    ws = torch.empty(pa.pillar_logprobs_workspace_bytes(0, 50, 2), dtype=torch.uint8, device=DEV)
+    none = lambda *shape, dtype=torch.float32: torch.zeros(*shape, dtype=dtype, device=DEV)
+    pa.pillar_token_logprobs(none(0, 50), ws, tokens=none(0, 2, dtype=torch.int32), logprobs=none(0, 2), lse=none(0), top_ids=none(0, 2, dtype=torch.int32), top_logprobs=none(0, 2))
+    torch.cuda.synchronize()

@@ -252,3 +252,37 @@ def test_a_workspace_asked_for_more_does_for_less():
     small.workspace = r.workspace
     small.run()
     check_prompt(small)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 8), (32, 2), (10, 2)])
+def test_few_rows_among_prompts(kv, Hq, Hkv):
+    """Requests on both sides of what counts as few rows, cut into ranges at any place."""
+    G = Hq // Hkv
+    new = [1, 64 // G, 64 // G + 1, 300, 2, 0, 150, 1]
+    r = PromptRun(make("few", 37, [1900, 700, 64 // G + 1, 300, 5, 40, 950, 1], Hq=Hq, Hkv=Hkv, D=128, kv=kv), new)
+    r.run()
+    check_prompt(r)
+
+
+def test_no_rows_and_no_tokens():
+    w = make("none", 38, [5, 9], Hq=4, Hkv=2, D=64)
+    r = PromptRun(w, [0, 0])
+    r.run()
+    assert torch.isnan(r.out).all() and torch.isnan(r.lse).all()
+    pa.pillar_prompt_attn(r.kv, r.q[:0], 1, r.out[:0], None, r.workspace, starts=r.starts_dev)
+    empty = PromptRun(make("empty", 39, [0, 0, 0], Hq=4, Hkv=2, D=64), [3, 0, 40])
+    empty.run()
+    check_prompt(empty)
+
+
+def test_bounds_that_are_far_above_the_lengths():
+    """max_seq_len and max_new choose kernels, and change nothing else."""
+    w = make("bounds", 40, [300, 40, 129], Hq=8, Hkv=2, D=64, extra_table_cols=600)
+    for most in (70, 5000):
+        r = PromptRun(w, [70, 33, 9])
+        r.kv.max_seq_len = 9000
+        r.most = most
+        r.workspace = torch.empty(pa.pillar_prompt_workspace_bytes(r.kv, r.q.shape[0], most), dtype=torch.uint8, device=DEV)
+        r.run()
+        check_prompt(r, str(most))

@@ -308,3 +308,46 @@ def test_captured_and_replayed_with_other_values(kv):
         torch.cuda.synchronize()
         a.rows = other.rows
         a.check()
+
+
+def test_nothing_to_do():
+    """No row at all, and requests of which none has a new token."""
+    w = make("nothing", 20, [20, 9], Hq=4, Hkv=2, D=64, kv="fp8_e4m3")
+    a = Append(w, [0, 0], r=64)
+    was = [t.clone() for t in (a.kv.k_pool, a.kv.v_pool, a.kv.k_scale, a.kv.v_scale)]
+    a.run()
+    pa.pillar_append_rotated(a.kv, a.rope, a.k[:0], a.v[:0], 1, starts=torch.zeros(3, dtype=torch.int32, device=DEV))
+    pa.pillar_rotate(a.q_out[:0], torch.zeros(0, dtype=torch.int32, device=DEV), a.rope, a.q_out[:0])
+    assert torch.isnan(a.q_out).all()
+    assert all(torch.equal(x.nan_to_num(-1), y.nan_to_num(-1)) if x.is_floating_point() else torch.equal(x, y)
+               for x, y in zip(was, (a.kv.k_pool, a.kv.v_pool, a.kv.k_scale, a.kv.v_scale)))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+def test_two_appends_at_once(kv):
+    """Two caches on two streams, each several times over."""
+    calls = [Append(make("at once", s, [300, 41, 90], Hq=4, Hkv=2, D=128, kv=kv), [200, 3, 90], seed=s, r=128) for s in (21, 22)]
+    was = [[t.clone() for t in (c.kv.k_pool, c.kv.v_pool, c.kv.k_scale, c.kv.v_scale) if t is not None] for c in calls]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    starts = [torch.tensor(c.starts, dtype=torch.int32, device=DEV) for c in calls]
+    for turn in range(4):
+        for c, before in zip(calls, was):
+            for t, x in zip([t for t in (c.kv.k_pool, c.kv.v_pool, c.kv.k_scale, c.kv.v_scale) if t is not None], before):
+                t.copy_(x)
+            c.q_out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for c, at, s in zip(calls, starts, streams):
+            pa.pillar_append_rotated(c.kv, c.rope, c.k, c.v, c.most, starts=at, q=c.q, q_out=c.q_out, stream=s)
+        torch.cuda.synchronize()
+        for c in calls:
+            c.check()
+
+
+def test_a_page_of_one_request_among_many_of_another_length():
+    """Pages are found by counting those of the requests before: lengths from none to many pages, more requests than lanes."""
+    rng = np.random.default_rng(23)
+    new = [int(n) for n in np.where(rng.random(130) < 0.3, 0, rng.integers(1, 80, 130))]
+    w = make("uneven", 23, [max(1, n + int(m)) for n, m in zip(new, rng.integers(-3, 40, 130))], Hq=2, Hkv=1, D=64, kv="fp8_e4m3")
+    a = Append(w, new, r=64)
+    a.run()
+    a.check()

@@ -201,3 +201,29 @@ def test_a_prompt_in_chunks_is_the_prompt(kv_dtype):
         f8 = lambda p: p.view(torch.float8_e4m3fn).float()
         for x, y in ((whole.k_pool, parts.k_pool), (whole.v_pool, parts.v_pool)):
             assert ((f8(x) - f8(y)).abs() <= 2.0 ** -3 * f8(x).abs() + 2.0 ** -9).all()
+
+
+@pytest.mark.parametrize("kv_dtype", ["bf16", "fp8_e4m3"])
+def test_pages_beyond_4_gib(kv_dtype):
+    """The same request in the first pages of a small pool and in the last ones of a large one: the same bits."""
+    fp8 = kv_dtype == "fp8_e4m3"
+    rng = np.random.default_rng(4)
+    T, heads, page = 300, 8, 256
+    rows = torch.from_numpy(rng.standard_normal((T, 2 * heads + heads, 128)).astype(np.float32)).bfloat16().to(DEV)
+    rope = pa.Rope(pa.pillar_rope_frequencies(128, 1e4)[0].to(DEV))
+
+    def run(pages):
+        pool = lambda: torch.zeros(pages, heads, page, 128, dtype=torch.uint8 if fp8 else torch.bfloat16, device=DEV)
+        scale = lambda: torch.zeros(pages, heads, device=DEV) if fp8 else None
+        kv = pa.KvCache(k_pool=pool(), v_pool=pool(), block_table=torch.tensor([[pages - 1, pages - 2]], dtype=torch.int32, device=DEV),
+                        seq_lens=torch.tensor([T], dtype=torch.int32, device=DEV), num_q_heads=heads, q_dtype="bf16", kv_dtype=kv_dtype, sm_scale=128 ** -0.5,
+                        max_seq_len=T, k_scale=scale(), v_scale=scale())
+        q = torch.empty(T, heads, 128, dtype=torch.bfloat16, device=DEV)
+        pa.pillar_append_rotated(kv, rope, rows[:, heads:2 * heads], rows[:, 2 * heads:], T, q=rows[:, :heads], q_out=q)
+        out, lse = torch.empty_like(q), torch.empty(T, heads, device=DEV)
+        pa.pillar_prompt_attn(kv, q, T, out, lse, torch.empty(pa.pillar_prompt_workspace_bytes(kv, T, T), dtype=torch.uint8, device=DEV))
+        return q, out, lse, kv.k_pool[[pages - 1, pages - 2]].clone(), kv.v_pool[[pages - 1, pages - 2]].clone()
+
+    small, large = run(2), run((5 << 30) // (heads * page * 128 * (1 if fp8 else 2)))
+    assert all(torch.equal(a, b) for a, b in zip(small, large))
+    assert small[1].isfinite().all() and (small[3].view(torch.float8_e4m3fn).float() if fp8 else small[3]).abs().max() > 0
