@@ -11,6 +11,9 @@
  *                         critical tokens of the next k draft steps;
  *   pillar_sparse_decode  draft attention that loads only the selected rows
  *                         (paged attention at page size 1, Section 4.2).
+ * and beside it, for the same cache: trees of drafted tokens, a cache that holds
+ * no more than a budget, and new tokens (rotary positions, the write into the
+ * cache, attention of prompts, what the logits say).
  *
  * Conventions shared by every entry point
  *   - Every pointer inside pillar_kv_t and every tensor argument is a DEVICE

@@ -10,6 +10,10 @@
 //                 (a step of one tile of one KV head) in a row are cut into equal ranges, one per resident workgroup; where a range ends
 //                 inside a tile it leaves a partial (m, l, O)
 //   prompt_merge  joins the partials
+//
+// Four prompts of 8 K tokens, 32 heads on 8: 2520 us, 871 TFLOP/s; two chunks of 2 K after 30 K 2220 us, 940 TFLOP/s, where a product of 8192^3 by the library runs at 1180.
+// Between the two lies what it takes to begin and end a tile.  (Two groups of wavefronts half a step apart, one at the products while the other takes
+// exponentials, gain nothing: 800 against 830 TFLOP/s at the time.)
 #include <algorithm>
 
 #include "host_rules.hpp"
