@@ -412,7 +412,8 @@ __global__ __launch_bounds__(kThreads) void logprob_join(Params p) {
 struct Plan {
   int parts, each;
 };
-// Two workgroups to a compute unit, in parts of 4096 bf16 or 2048 fp32 logits at the least.
+// Two workgroups to a compute unit, in parts of 4096 bf16 or 2048 fp32 logits at the least: shorter parts are more lists to join, longer ones take longer.  One row of
+// 150000 bf16 logits with eight alternatives, parts of 2048 / 4096 / 8192 / 16384: 17.1 / 13.6 / 13.4 / 15.7 us, of 32000 11.6 / 10.9 / 12.2 / 14.6.
 Plan plan_of(int rows, int vocab, int dtype) {
   const int per = dtype == PILLAR_F32 ? 4 : 8, vectors = vocab / per;
   const int64_t wanted = (2 * static_cast<int64_t>(num_cus()) + rows - 1) / std::max(rows, 1);
