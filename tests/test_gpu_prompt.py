@@ -286,3 +286,36 @@ def test_bounds_that_are_far_above_the_lengths():
         r.workspace = torch.empty(pa.pillar_prompt_workspace_bytes(r.kv, r.q.shape[0], most), dtype=torch.uint8, device=DEV)
         r.run()
         check_prompt(r, str(most))
+
+
+def test_queries_and_results_at_any_address():
+    """Rows that are not at multiples of 16 bytes: fp32 arithmetic, one element at a time."""
+    r = PromptRun(make("address", 41, [90, 33], Hq=4, Hkv=2, D=64), [50, 33])
+    for name in ("q", "out"):
+        t = getattr(r, name)
+        at = torch.full((t.numel() + 3,), float("nan"), dtype=t.dtype, device=DEV)[3:].view(t.shape)
+        at.copy_(t)
+        setattr(r, name, at)
+    r.run()
+    check_prompt(r)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+def test_replayed_with_other_lengths(kv):
+    """Lengths and starts are on the device: a captured call works out its share of the work anew."""
+    w = make("lengths", 42, [900, 500, 40, 300], Hq=16, Hkv=4, D=128, kv=kv)
+    r = PromptRun(w, [300, 1, 40, 64])
+    r.run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.run()
+    for lens, new in (([900, 500, 40, 300], [300, 1, 40, 64]), ([17, 400, 0, 299], [2, 280, 3, 100]), ([880, 1, 33, 64], [0, 1, 33, 64])):
+        w.seq_lens[:] = lens
+        r.starts = [sum(new[:b]) for b in range(5)]
+        r.kv.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        r.starts_dev.copy_(torch.tensor(r.starts, dtype=torch.int32))
+        r.out.fill_(float("nan")), r.lse.fill_(float("nan")), r.workspace.fill_(77)
+        g.replay()
+        torch.cuda.synchronize()
+        check_prompt(r, str(lens))
