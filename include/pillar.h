@@ -428,7 +428,7 @@ int pillar_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, do
  *   x    device [tokens][num_heads][head_dim] of `dtype` (PILLAR_F32 | PILLAR_BF16), token t at element t * x_stride (x_stride >= num_heads *
  *        head_dim: rows of a fused projection will do), heads dense within; out likewise.
  *   positions  device [tokens] int32.
- * out may be x itself with the same stride; else the two spans must not overlap (PILLAR_EINVAL).  head_dim 2..512, even. */
+ * out may be x itself with the same stride; else the two spans must not overlap (PILLAR_EINVAL).  head_dim 2..512, even; at most 2^24 - 1 tokens. */
 int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_heads, int32_t head_dim, int32_t dtype,
                   const int32_t* positions, const pillar_rope_t* rope, void* out, int64_t out_stride, void* hip_stream);
 
@@ -448,7 +448,8 @@ int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_h
  * those nearest to value * (1 / scale), infinities becoming the largest code (NaN in a page of scale 0), NaN staying NaN.  A page without older
  * tokens takes the new ones' scale alone.
  * Tokens whose number would be negative are skipped (their queries are rotated all the same).  No page that receives rows may belong to
- * two requests.  Bases and strides of pools, q, k_new, v_new and q_out in multiples of 16 bytes, else PILLAR_EUNSUPPORTED. */
+ * two requests.  Bases and strides of pools, q, k_new, v_new and q_out in multiples of 16 bytes, and at most 2^24 - 1 rows (for fp8: rows of
+ * queries and pages with new rows times KV heads), else PILLAR_EUNSUPPORTED. */
 int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, const int32_t* starts, int32_t total_rows, int32_t max_new,
                           const int32_t* positions, const void* q, int64_t q_stride, void* q_out,
                           const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* hip_stream);
@@ -485,6 +486,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
  * Logits of -inf (masked tokens) have probability 0 and add nothing to the entropy.  A row of nothing else: lse = -inf, all log probabilities
  * -inf, entropy 0.  NaN makes the row's lse, log probabilities and entropy NaN, but it is nobody's alternative before all numbers, -inf among
  * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Everything is summed in fp32 relative to the row's maximum.
+ * At most 2^24 - 1 rows, 2^30 logits and 2^30 given tokens in each (PILLAR_EUNSUPPORTED).
  * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments). */
 size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, float scale,

@@ -11,6 +11,8 @@ namespace pillar {
 constexpr int kWave = 64;
 constexpr int kMaxRows = 64;      // (k+1)*G rows of one KV head at most
 constexpr int kMostAlternatives = 64;   // of a row of logits
+constexpr int kMostTokens = 1 << 30;    // of a row of logits, or asked for of it: numbers stay in 32 bits also a workgroup's step past the end
+constexpr int kMostGroups = (1 << 24) - 1;      // workgroups of 256 threads in a launch: work-items are counted in 32 bits
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -647,7 +647,7 @@ int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_h
                   const pillar_rope_t* rope, void* out, int64_t out_stride, void* hip_stream) {
   if (tokens < 0 || num_heads < 1 || head_dim < 2 || head_dim % 2 != 0) return PILLAR_EINVAL;
   if (dtype != PILLAR_F32 && dtype != PILLAR_BF16) return PILLAR_EUNSUPPORTED;
-  if (head_dim > 512 || num_heads > 65535) return PILLAR_EUNSUPPORTED;
+  if (head_dim > 512 || num_heads > 65535 || tokens > kMostGroups) return PILLAR_EUNSUPPORTED;
   if (!rope || (tokens > 0 && (!x || !positions || !out))) return PILLAR_EINVAL;
   const int64_t row = static_cast<int64_t>(num_heads) * head_dim;
   if (x_stride < row || out_stride < row) return PILLAR_EINVAL;
@@ -754,7 +754,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
 }
 
 size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
-  if (rows < 0 || vocab < 1 || top < 0 || top > kMostAlternatives) return 0;
+  if (rows < 0 || rows > kMostGroups || vocab < 1 || vocab > kMostTokens || top < 0 || top > kMostAlternatives) return 0;
   return std::max<size_t>(256, logprobs_workspace(rows, vocab, top));
 }
 
@@ -764,7 +764,7 @@ int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32
   if (rows < 0 || vocab < 1 || row_stride < vocab || num_tokens < 0 || top < 0) return PILLAR_EINVAL;
   if (!(scale > 0.f) || !(scale < 1e30f)) return PILLAR_EINVAL;
   if (dtype != PILLAR_F32 && dtype != PILLAR_BF16) return PILLAR_EUNSUPPORTED;
-  if (top > kMostAlternatives) return PILLAR_EUNSUPPORTED;
+  if (top > kMostAlternatives || rows > kMostGroups || vocab > kMostTokens || num_tokens > kMostTokens) return PILLAR_EUNSUPPORTED;
   if (rows == 0) return PILLAR_OK;
   if (!logits) return PILLAR_EINVAL;
   if ((num_tokens > 0) != (tokens != nullptr) || (num_tokens > 0) != (logprobs != nullptr)) return PILLAR_EINVAL;

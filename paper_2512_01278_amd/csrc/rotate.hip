@@ -390,7 +390,7 @@ hipError_t append_as(const AppendArgs& a, hipStream_t s) {
 
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) { return a.dtype == PILLAR_F32 ? rotate_as<PILLAR_F32>(a, s) : rotate_as<PILLAR_BF16>(a, s); }
 
-bool append_fits_a_grid(const AppendArgs& a) { return a.kv_dtype != PILLAR_FP8_E4M3 || pages_of(a).workgroups <= INT32_MAX; }
+bool append_fits_a_grid(const AppendArgs& a) { return (a.kv_dtype == PILLAR_FP8_E4M3 ? pages_of(a).workgroups : a.total_rows) <= kMostGroups; }
 
 hipError_t launch_append_rotated(const AppendArgs& a, hipStream_t s) {
   return a.q_dtype == PILLAR_F32 ? append_as<PILLAR_F32>(a, s) : append_as<PILLAR_BF16>(a, s);

@@ -254,6 +254,25 @@ def test_logprobs_refuse(lib):
     assert need(-1, 10, 1) == 0 and need(1, 0, 1) == 0 and need(1, 10, -1) == 0 and need(1, 10, 65) == 0 and need(0, 10, 0) > 0
 
 
+def test_more_than_a_grid_or_32_bits_hold_is_refused(lib):
+    """Work-items of a launch are counted in 32 bits, 256 to a workgroup; numbers of logits and given tokens in 32 bits with a sign, also a step past the end."""
+    groups, tokens, room = 1 << 24, (1 << 30) + 1, 1 << 60
+    assert lib.pillar_rotate(FAKE, 128, groups, 1, 128, pb.PILLAR_BF16, FAKE, C.byref(rope()), FAKE, 128, None) == UNSUPPORTED
+    fp8 = dict(kv_dtype=pb.PILLAR_FP8_E4M3, k_scale=FAKE, v_scale=FAKE)
+
+    def append(kv, rows, q=None):
+        return lib.pillar_append_rotated(C.byref(kv), None, FAKE, rows, 1 << 28, None, q, 4096, q and 1 << 50, 1 << 52, 1024, 1 << 54, 1024, None)
+    assert append(good_kv(), groups) == UNSUPPORTED and append(good_kv(**fp8), groups, FAKE) == UNSUPPORTED
+    assert append(good_kv(max_seq_len=1 << 28, block_table_stride=1 << 24, **fp8), 1 << 28) == UNSUPPORTED         # 2^24 pages and more, without queries
+    need = lib.pillar_logprobs_workspace_bytes
+
+    def call(rows=1, vocab=10, m=0):
+        return lib.pillar_token_logprobs(FAKE, pb.PILLAR_BF16, rows, vocab, vocab, 1.0, m and FAKE, m, m and 1 << 50, None, None, 0, None, None, FAKE, room, None)
+    for bad in (dict(rows=groups), dict(vocab=tokens), dict(m=tokens), dict(rows=2**31 - 1), dict(vocab=2**31 - 1), dict(m=2**31 - 1)):
+        assert call(**bad) == UNSUPPORTED, bad
+    assert need(groups, 10, 1) == 0 and need(1, tokens, 1) == 0 and need(groups - 1, 10, 1) > 0 and need(1, tokens - 1, 1) > 0
+
+
 def cpu_cache(q="bf16", kv="bf16"):
     pool = torch.zeros(8, 2, 16, 64, dtype={"bf16": torch.bfloat16, "f32": torch.float32}[kv])
     return pa.KvCache(k_pool=pool, v_pool=pool.clone(), block_table=torch.zeros(2, 4, dtype=torch.int32), seq_lens=torch.zeros(2, dtype=torch.int32),
