@@ -486,6 +486,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
  * Logits of -inf (masked tokens) have probability 0 and add nothing to the entropy.  A row of nothing else: lse = -inf, all log probabilities
  * -inf, entropy 0.  NaN makes the row's lse, log probabilities and entropy NaN, but it is nobody's alternative before all numbers, -inf among
  * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Everything is summed in fp32 relative to the row's maximum.
+ * No output may overlap logits or tokens, which others of a row's threads still read (PILLAR_EINVAL).
  * At most 2^24 - 1 rows, 2^30 logits and 2^30 given tokens in each (PILLAR_EUNSUPPORTED).
  * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments). */
 size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);

@@ -773,6 +773,11 @@ int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32
   if (reinterpret_cast<uintptr_t>(logits) % esz != 0) return PILLAR_EUNSUPPORTED;
   const int rc = check_workspace(workspace, workspace_bytes, pillar_logprobs_workspace_bytes(rows, vocab, top));
   if (rc != PILLAR_OK) return rc;
+  // a row's threads look at its logits and tokens until its last result is written
+  const uint64_t read = span_of(rows, row_stride, vocab, static_cast<int>(esz)), asked = 4ull * rows * num_tokens, listed = 4ull * rows * top;
+  const std::pair<const void*, uint64_t> outs[] = {{logprobs, asked}, {lse, 4ull * rows}, {entropy, 4ull * rows}, {top_ids, listed}, {top_logprobs, listed}};
+  for (const auto& o : outs)
+    if (o.first && (overlap(logits, read, o.first, o.second) || (tokens && overlap(tokens, asked, o.first, o.second)))) return PILLAR_EINVAL;
   LogprobArgs a;
   a.logits = logits;
   a.dtype = dtype;

@@ -273,6 +273,16 @@ def test_more_than_a_grid_or_32_bits_hold_is_refused(lib):
     assert need(groups, 10, 1) == 0 and need(1, tokens, 1) == 0 and need(groups - 1, 10, 1) > 0 and need(1, tokens - 1, 1) > 0
 
 
+def test_results_over_logits_or_tokens_are_refused(lib):
+    rows, vocab, m, top = 3, 1000, 5, 4
+    x, tok, apart = FAKE, 2 * FAR, [(3 + i) * FAR for i in range(5)]
+    for at in range(5):
+        size = 4 * rows * (m, 1, 1, top, top)[at]
+        for bad in (x, x + 2 * rows * vocab - 4, x - size + 4, tok, tok + 4 * rows * m - 4, tok - size + 4):
+            o = [bad if i == at else apart[i] for i in range(5)]
+            assert lib.pillar_token_logprobs(x, pb.PILLAR_BF16, rows, vocab, vocab, 1.0, tok, m, *o[:3], top, *o[3:], 20 * FAR, 1 << 30, None) == INVALID, (at, bad)
+
+
 def cpu_cache(q="bf16", kv="bf16"):
     pool = torch.zeros(8, 2, 16, 64, dtype={"bf16": torch.bfloat16, "f32": torch.float32}[kv])
     return pa.KvCache(k_pool=pool, v_pool=pool.clone(), block_table=torch.zeros(2, 4, dtype=torch.int32), seq_lens=torch.zeros(2, dtype=torch.int32),
