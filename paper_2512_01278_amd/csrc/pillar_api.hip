@@ -739,7 +739,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
   if (total_rows == 0) return PILLAR_OK;
   // several workgroups read a row of q, and one of them writes its result
   const uint64_t bytes = static_cast<uint64_t>(total_rows) * kv->num_q_heads * kv->head_dim * (kv->q_dtype == PILLAR_F32 ? 4 : 2);
-  if (overlap(q, bytes, out, bytes)) return PILLAR_EINVAL;
+  if (overlap(q, bytes, out, bytes) || (lse && overlap(q, bytes, lse, 4ull * total_rows * kv->num_q_heads))) return PILLAR_EINVAL;
   a.q = q;
   a.starts = starts;
   a.total_rows = total_rows;

@@ -228,6 +228,11 @@ def test_prompt_refuses(lib):
     assert need(T=-1) == 0 and need(most=0) == 0 and need(good_kv(batch=0)) == 0 and need() > 0
 
 
+def test_lse_over_the_queries_is_refused(lib):
+    for lse in (FAKE, FAKE + 1000 * 32 * 128 * 2 - 4, FAKE - 1000 * 32 * 4 + 4):
+        assert lib.pillar_prompt_attn(C.byref(good_kv()), FAKE, FAKE, 1000, 500, FAR, lse, 2 * FAR, 1 << 40, None) == INVALID, lse
+
+
 def test_workspace_of_a_prompt_does_for_smaller_ones(lib):
     need = lambda T, most, B=4, top=1024: lib.pillar_prompt_workspace_bytes(C.byref(good_kv(batch=B, max_seq_len=top)), T, most)
     for T, most, B, top in ((1, 1, 1, 1), (4, 1, 4, 1024), (100, 30, 4, 700), (1000, 1000, 1, 1000)):
