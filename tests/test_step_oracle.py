@@ -229,8 +229,9 @@ def test_prompt_refuses(lib):
 
 
 def test_lse_over_the_queries_is_refused(lib):
-    for lse in (FAKE, FAKE + 1000 * 32 * 128 * 2 - 4, FAKE - 1000 * 32 * 4 + 4):
-        assert lib.pillar_prompt_attn(C.byref(good_kv()), FAKE, FAKE, 1000, 500, FAR, lse, 2 * FAR, 1 << 40, None) == INVALID, lse
+    q = 4 * FAR                # (room for lse below it: an address does not go below 0)
+    for lse in (q, q + 1000 * 32 * 128 * 2 - 4, q - 1000 * 32 * 4 + 4):
+        assert lib.pillar_prompt_attn(C.byref(good_kv()), q, FAKE, 1000, 500, FAR, lse, 2 * FAR, 1 << 40, None) == INVALID, lse
 
 
 def test_workspace_of_a_prompt_does_for_smaller_ones(lib):
