@@ -485,7 +485,9 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
  *   lse, entropy: device [rows] fp32, each may be NULL.  top 0..64; top_ids and top_logprobs NULL exactly if top is 0.
  * Logits of -inf (masked tokens) have probability 0 and add nothing to the entropy.  A row of nothing else: lse = -inf, all log probabilities
  * -inf, entropy 0.  NaN makes the row's lse, log probabilities and entropy NaN, but it is nobody's alternative before all numbers, -inf among
- * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Everything is summed in fp32 relative to the row's maximum.
+ * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Sums are fp32, of shares relative to one of the largest logits, whose own share is
+ * kept apart: the log probability of a nearly certain token, and the entropy beside it, are exact to 10^-5 of themselves
+ * (at the worst 2^-24 more for every 2048 logits beyond ten thousand).
  * No output may overlap logits or tokens, which others of a row's threads still read (PILLAR_EINVAL).
  * At most 2^24 - 1 rows, 2^30 logits and 2^30 given tokens in each (PILLAR_EUNSUPPORTED).
  * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments). */

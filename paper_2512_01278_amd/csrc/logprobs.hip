@@ -1,9 +1,12 @@
 // What rows of logits say about given tokens: log-sum-exp, log probabilities, entropy, the tokens of largest logit.
 //
-// With c = scale log2 e and m the largest logit so far, y = (x - m) c:   S = sum 2^y,  A = sum 2^y y,
-//   lse = scale m + ln 2 log2 S,  log p = scale (x - m) - ln 2 log2 S,  entropy = ln 2 (log2 S - A / S)
-// so one pass over the row does (when m moves, S and A are carried over: with d = (m - m') c, S' = 2^d S, A' = 2^d (A + d S)).  Everything is a
-// difference against the row's own maximum and loses nothing to its size: a row of nothing but -3e38, as masks have it, is as any other row of equal logits.
+// With c = scale log2 e, m one of the largest logits so far, y = (x - m) c:   R = sum of 2^y over all others,  A = sum of 2^y y over them,
+//   lse = scale m + log(1 + R),  log p = scale (x - m) - log(1 + R),  entropy = log(1 + R) - ln 2 A / (1 + R)
+// so one pass over the row does (when m moves to m', with d = (m - m') c:  R' = 2^d (1 + R),  A' = 2^d (A + d (1 + R)), and the new m stays out).  Everything is a
+// difference against a logit of the row and loses nothing to its size: a row of nothing but -3e38, as masks have it, is as any other row of equal logits.
+//
+// The 1 of m is never added to the rest.  Of a token that is nearly certain, 1 + R would keep what of R lies above 2^-24, while log(1 + R) and the entropy are
+// hardly more than R: 10^-4 of themselves off at 1 - p = 10^-3.  Apart from it they are exact to 10^-5 of themselves, however small.
 //
 //   logprob_pass   a workgroup per (row, part of the row): (M, S, A) and the `top` largest of the part
 //   logprob_join   a workgroup per row: joins the parts, looks the given tokens up
@@ -27,23 +30,22 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
+// No logit is further (log2) above the reference m than this.  A first token of more than p = 4/5 is the reference, then; with less, R is 1/4 and more and
+// nothing is lost in 1 + R.  A move takes a wavefront as long as a batch does: with every new largest 640 rows of 150000 took 50.8 us, so 46.9.
+constexpr float kRoom = 2.f;
+
+
 struct Sums {
-  float m, s, a;               // m = -inf: nothing but -inf so far
-  // moves the maximum up to `to`
-  __device__ __forceinline__ void move(float to, float c) {
-    if (m == to) return;                                 // (also: both -inf)
-    const float d = (m - to) * c;                        // -inf: nothing there
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
-    a = f == 0.f ? 0.f : f * (a + d * s);
-    s = f == 0.f && !(s != s) ? 0.f : f * s;
-    m = to;
-  }
+  float m, s, a;               // largest logit (-inf: none so far), R (NaN: there was one), A
+  // The one with the smaller maximum comes over with its largest, whose share is 1.
   __device__ __forceinline__ void add(Sums o, float c) {
-    const float top = fmaxf(m, o.m);
-    move(top, c);
-    o.move(top, c);
-    s += o.s;
-    a += o.a;
+    const bool mine = m >= o.m;
+    const float top = mine ? m : o.m, low = mine ? o.m : m;
+    const float d = top == low ? 0.f : (low - top) * c, f = low == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+    const float t = (low == -INFINITY ? 0.f : 1.f) + (mine ? o.s : s);
+    s = __builtin_fmaf(f, t, mine ? s : o.s);
+    a = (mine ? a : o.a) + (f == 0.f ? 0.f : f * __builtin_fmaf(d, t, mine ? o.a : a));
+    m = top;
   }
 };
 
@@ -103,24 +105,39 @@ struct List {
   }
 };
 
+// (the same in all lanes)
+template <int O = 32>
+__device__ __forceinline__ float over_lanes_max(float x) {
+  x = fmaxf(x, lane_xor<O>(x));
+  if constexpr (O > 1) return over_lanes_max<O / 2>(x);
+  else return __uint_as_float(__builtin_amdgcn_readfirstlane(static_cast<int>(__float_as_uint(x))));
+}
+template <int O = 32>
+__device__ __forceinline__ float over_lanes_sum(float x) {
+  x += lane_xor<O>(x);
+  if constexpr (O > 1) return over_lanes_sum<O / 2>(x);
+  else return x;
+}
+
 template <int DT>
 __device__ __forceinline__ float logit(const void* p, int64_t i) { return Storage<DT>::load(p, i); }
 
 constexpr int kLoads = 2, kAhead = 2;                    // 16-byte loads of a lane in a batch, batches on their way
 constexpr int kFew = 8;                                  // what is put into a list one by one rather than sorted
 
-// One wavefront's share of a row.
+// One wavefront's share of a row.  (m: the same in all its lanes, so that the one that stays out is the wavefront's.)
 template <int DT, bool TOP>
 struct Scan {
   static constexpr int V = DT == PILLAR_F32 ? 4 : 8, kBatch = kLoads * V;
-  Sums sums;
+  Sums sums;                   // m: the same in all lanes; s, a: of this lane
+  float limit, room;           // what a logit has to exceed to become the reference; how far above that this is
   List list;
   float least;                 // the list's last of `top`
   Key least_key;
   float c;
   int top, lane;
 
-  __device__ __forceinline__ Scan(float c_, int top_) : sums{-INFINITY, 0.f, 0.f}, least(-INFINITY), least_key(0), c(c_), top(top_), lane(threadIdx.x & 63) {}
+  __device__ __forceinline__ Scan(float c_, int top_) : sums{-INFINITY, 0.f, 0.f}, limit(-INFINITY), room(fminf(kRoom / c_, 1e37f)), least(-INFINITY), least_key(0), c(c_), top(top_), lane(threadIdx.x & 63) {}
 
   // What of N logits of every lane gets into the list.  Each lane brings its best (`most`), then its next best as long as some get in: one by one where
   // they are few, else sorted and merged at once.
@@ -158,17 +175,9 @@ struct Scan {
     }
   }
 
-  // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th.  LATER: all of them higher than those before.
-  template <bool LATER, int N, typename Id>
-  __device__ __forceinline__ void take(float (&x)[N], Id id) {
-    float most = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
-    // the reference moves only for a logit that exceeds it by more than 8 (log2): 2^y stays below 2^8
-    const bool moves = (most - sums.m) * c > 8.f || (sums.m == -INFINITY && most > -INFINITY);
-    if (__any(moves)) {
-      if (moves) sums.move(most, c);
-    }
+  // logits into the sums
+  template <int N>
+  __device__ __forceinline__ void weigh(const float (&x)[N]) {
     const float m = sums.m == -INFINITY ? 0.f : sums.m;
     float s[2] = {0.f, 0.f}, a[2] = {0.f, 0.f};
 #pragma unroll
@@ -179,6 +188,36 @@ struct Scan {
     }
     sums.s += s[0] + s[1];
     sums.a += a[0] + a[1];
+  }
+
+  // N logits of every lane, -inf where there is none; id(i): the number of a lane's i-th.  LATER: all of them higher than those before.
+  template <bool LATER, int N, typename Id>
+  __device__ __forceinline__ void take(float (&x)[N], Id id) {
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+    // A logit far enough above the reference becomes it (rare after a few batches): it stays out of the sums, and the one before goes into them, in lane 0.
+    if (__any(most > limit)) {
+      const float to = over_lanes_max(most), d = (sums.m - to) * c, f = sums.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+      const float t = sums.s + (lane == 0 && f > 0.f ? 1.f : 0.f);
+      sums.a = f == 0.f ? 0.f : f * __builtin_fmaf(d, t, sums.a);
+      sums.s = f * t;
+      sums.m = to;
+      limit = to + room;
+      const bool mine = lane == __builtin_ctzll(__ballot(most == to));
+      float equal = mine ? -1.f : 0.f;                   // others of the lane that are as large
+      float rest[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const bool same = mine && x[i] == to;
+        rest[i] = same ? -INFINITY : x[i];
+        equal += same ? 1.f : 0.f;
+      }
+      sums.s += equal;
+      weigh(rest);
+    } else {
+      weigh(x);
+    }
     if constexpr (TOP) {
       if (__any(LATER ? most > least : most >= least)) enter(x, id, most);
     }
@@ -229,14 +268,14 @@ struct Row {
   int r;
   int64_t at;                  // its first element
   Sums sums;
-  float log_s;                 // in natural units
+  float log_s;                 // log(1 + R), in natural units
   bool nan, empty, endless;
 
   __device__ __forceinline__ Row(const LogprobArgs& a_, int r_) : a(a_), r(r_), at(r_ * a_.row_stride) {}
-  // (all threads of a workgroup) m = -inf: nothing but -inf (and NaN); +inf: the sum is NaN, from inf - inf, and whether the row has NaN too has to be looked up
+  // (all threads of a workgroup) m = -inf: nothing but -inf (and NaN); +inf: the sum may be NaN from inf - inf, and whether the row has NaN too has to be looked up
   __device__ __forceinline__ void settle(Sums s) {
     sums = s;
-    log_s = kLn2 * log2f(s.s);
+    log_s = log1pf(s.s);
     endless = s.m == INFINITY, empty = s.m == -INFINITY;
     nan = s.s != s.s;
     if (endless) {
@@ -266,8 +305,7 @@ struct Row {
   }
   __device__ __forceinline__ void put_sums() const {
     if (a.lse) a.lse[r] = nan ? NAN : empty ? -INFINITY : endless ? INFINITY : __builtin_fmaf(a.scale, sums.m, log_s);
-    const float h = log_s - kLn2 * (sums.a / sums.s);    // (a little below 0 by rounding where one token has it all)
-    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty || h < 0.f ? 0.f : h;
+    if (a.entropy) a.entropy[r] = nan || endless ? NAN : empty ? 0.f : log_s - kLn2 * (sums.a / (1.f + sums.s));        // (a sum: A is not positive)
   }
   // (one wavefront) Fewer numbers above -inf than wanted: the first of -inf, then the first that are none at all.
   __device__ __forceinline__ void put_list(List list) const {
@@ -333,7 +371,7 @@ __global__ __launch_bounds__(kThreads) void logprob_pass(Params p) {
     float x[1] = {lane < head + rest ? logit<DT>(a.logits, row.at + id) : -INFINITY};
     scan.template take<false>(x, [&](int) { return id; });
   }
-  const Sums sums = over_lanes(scan.sums, p.c);
+  const Sums sums{scan.sums.m, over_lanes_sum(scan.sums.s), over_lanes_sum(scan.sums.a)};
   if (lane == 0) s_sums[wave] = sums;
   List list = scan.list;
   if (TOP) merge_lists(list, s_key, wave, lane);
