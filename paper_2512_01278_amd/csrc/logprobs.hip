@@ -35,13 +35,16 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr float kRoom = 2.f;
 
 
+// Half of x - m, which itself may be more than fp32 holds (logits of either sign near the type's end, under a small scale); factors on it are doubled.
+__device__ __forceinline__ float half_apart(float x, float m) { return __builtin_fmaf(x, 0.5f, -0.5f * m); }
+
 struct Sums {
   float m, s, a;               // largest logit (-inf: none so far), R (NaN: there was one), A
   // The one with the smaller maximum comes over with its largest, whose share is 1.
   __device__ __forceinline__ void add(Sums o, float c) {
     const bool mine = m >= o.m;
     const float top = mine ? m : o.m, low = mine ? o.m : m;
-    const float d = top == low ? 0.f : (low - top) * c, f = low == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+    const float d = top == low ? 0.f : half_apart(low, top) * (2.f * c), f = low == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
     const float t = (low == -INFINITY ? 0.f : 1.f) + (mine ? o.s : s);
     s = __builtin_fmaf(f, t, mine ? s : o.s);
     a = (mine ? a : o.a) + (f == 0.f ? 0.f : f * __builtin_fmaf(d, t, mine ? o.a : a));
@@ -182,7 +185,7 @@ struct Scan {
     float s[2] = {0.f, 0.f}, a[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float y = (x[i] - m) * c, e = __builtin_amdgcn_exp2f(y);
+      const float y = half_apart(x[i], m) * (2.f * c), e = __builtin_amdgcn_exp2f(y);
       s[i & 1] += e;
       a[i & 1] = __builtin_fmaf(e, fmaxf(y, -200.f), a[i & 1]);          // (-inf: 0 * -200)
     }
@@ -198,7 +201,7 @@ struct Scan {
     for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
     // A logit far enough above the reference becomes it (rare after a few batches): it stays out of the sums, and the one before goes into them, in lane 0.
     if (__any(most > limit)) {
-      const float to = over_lanes_max(most), d = (sums.m - to) * c, f = sums.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+      const float to = over_lanes_max(most), d = half_apart(sums.m, to) * (2.f * c), f = sums.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
       const float t = sums.s + (lane == 0 && f > 0.f ? 1.f : 0.f);
       sums.a = f == 0.f ? 0.f : f * __builtin_fmaf(d, t, sums.a);
       sums.s = f * t;
@@ -291,7 +294,7 @@ struct Row {
     if (nan) return NAN;
     if (empty) return -INFINITY;
     if (endless) return x < INFINITY ? -INFINITY : NAN;
-    return __builtin_fmaf(x - sums.m, a.scale, -log_s);
+    return __builtin_fmaf(half_apart(x, sums.m), 2.f * a.scale, -log_s);
   }
   // the j-th given token: its logit, or NaN where there is no such token
   __device__ __forceinline__ bool given(int j, float& x) const {

@@ -119,3 +119,15 @@ def test_rising_and_falling():
     x = torch.stack([up, up.flip(0), up, up.flip(0)])
     x[2, -1], x[3, 0] = 0.0, 0.0
     check(x, 1.0, tokens_of(4, V, V - 1, np.zeros(4, dtype=int), 5), 2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 9000, 50000])
+def test_logits_further_apart_than_their_type_reaches(dtype, V):
+    """x - m is beyond the largest number while scale * (x - m) is not."""
+    x = torch.full((3, V), -3.0e38, dtype=QT[dtype])
+    x[:, V // 2], x[:, 3] = 3.0e38, 0.0
+    x[1, 5:20] = 2.5e38
+    x[2, ::2] = -1.0e38
+    scale = 4.0e-38 if V < 100 else 6.0e-38
+    check(x, scale, tokens_of(3, V, V // 2, np.array([3, 7, 4]), V), 3)
