@@ -490,7 +490,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
  * (at the worst 2^-24 more for every 2048 logits beyond ten thousand).
  * No output may overlap logits or tokens, which others of a row's threads still read (PILLAR_EINVAL).
  * At most 2^24 - 1 rows, 2^30 logits and 2^30 given tokens in each (PILLAR_EUNSUPPORTED).
- * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments). */
+ * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments), enough for fewer rows, smaller vocabularies and fewer alternatives too. */
 size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, float scale,
                           const int32_t* tokens, int32_t num_tokens, float* logprobs, float* lse, float* entropy,

@@ -455,9 +455,10 @@ struct Plan {
 };
 // Two workgroups to a compute unit, in parts of 4096 bf16 or 2048 fp32 logits at the least: shorter parts are more lists to join, longer ones take longer.  One row of
 // 150000 bf16 logits with eight alternatives, parts of 2048 / 4096 / 8192 / 16384: 17.1 / 13.6 / 13.4 / 15.7 us, of 32000 11.6 / 10.9 / 12.2 / 14.6.
+int64_t wanted_workgroups() { return 2 * static_cast<int64_t>(num_cus()); }
 Plan plan_of(int rows, int vocab, int dtype) {
   const int per = dtype == PILLAR_F32 ? 4 : 8, vectors = vocab / per;
-  const int64_t wanted = (2 * static_cast<int64_t>(num_cus()) + rows - 1) / std::max(rows, 1);
+  const int64_t wanted = (wanted_workgroups() + rows - 1) / std::max(rows, 1);
   const int most = (vectors + 511) / 512;
   Plan p;
   p.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(wanted, most)));
@@ -480,10 +481,12 @@ hipError_t launch(const Params& p, hipStream_t s) {
 
 }  // namespace
 
-// (whatever the type)
+// Whatever the type, and enough for any smaller call: r rows have at most r * most parts, and fewer than the wanted workgroups and one more for each row; as many
+// rows as workgroups are wanted have one part each, which leaves nothing.
 size_t logprobs_workspace(int rows, int vocab, int top) {
-  const size_t parts = std::max(plan_of(rows, vocab, PILLAR_F32).parts, plan_of(rows, vocab, PILLAR_BF16).parts);
-  return align_up(rows * parts * 16, 256) + rows * parts * top * 8;
+  const int64_t most = (vocab / 4 + 511) / 512, few = std::min<int64_t>(rows, wanted_workgroups() - 1);
+  const size_t slots = most > 1 ? std::min(few * most, wanted_workgroups() + few - 1) : 0;
+  return align_up(slots * 16, 256) + slots * top * 8;
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {

@@ -131,3 +131,21 @@ def test_logits_further_apart_than_their_type_reaches(dtype, V):
     x[2, ::2] = -1.0e38
     scale = 4.0e-38 if V < 100 else 6.0e-38
     check(x, scale, tokens_of(3, V, V // 2, np.array([3, 7, 4]), V), 3)
+
+
+def test_a_workspace_for_many_rows_does_for_fewer():
+    """One of the largest call's size, with nothing written behind it."""
+    V, top = 50000, 8
+    size = pa.pillar_logprobs_workspace_bytes(640, V, top)
+    ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device=DEV)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = (torch.randn(640, V, generator=torch.Generator().manual_seed(5)) * 3).to(dtype).to(DEV)
+        whole = torch.empty(640, top, device=DEV)
+        pa.pillar_token_logprobs(x, ws[:size], top_ids=torch.empty(640, top, dtype=torch.int32, device=DEV), top_logprobs=whole)
+        for R in (511, 300, 255, 171, 64, 3, 1):
+            ids, lp, lse = torch.empty(R, top, dtype=torch.int32, device=DEV), torch.empty(R, top, device=DEV), torch.empty(R, device=DEV)
+            pa.pillar_token_logprobs(x[:R], ws[:size], lse=lse, top_ids=ids, top_logprobs=lp)
+            # (other parts, other sums: 2^-24 for each of some 60 additions and of an exponent below 40)
+            assert ((lp - whole[:R]).abs() <= 200 * 2.0 ** -24 * whole[:R].abs().clamp(min=1.0)).all(), R
+            assert torch.equal(ids[:, 0].long(), x[:R].float().argmax(dim=1)), R
+    assert (ws[size:] == 77).all()
