@@ -445,8 +445,9 @@ int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_h
  * The cache may have any of its types: values are rounded once, to nearest even, from the fp32 result.  WRITES into the pools and, for fp8,
  * into k_scale and v_scale: a page gets the largest scale of its older tokens' (those before the new ones; their codes are rounded anew where it
  * grew, as by pillar_tree_commit) and what the new ones need, max |finite new value| / 448, or 0 where that maximum is below 2^-90; codes are
- * those nearest to value * (1 / scale), infinities becoming the largest code (NaN in a page of scale 0), NaN staying NaN.  A page without older
- * tokens takes the new ones' scale alone.
+ * those nearest to value * (1 / scale), infinities becoming the largest code, NaN staying NaN; in a page whose scale is 0, or stays below 2^-90 / 448 (that of
+ * older tokens next to nothing, beside new ones that are no more), they are zeros, and NaN for what is not finite.  A page without older tokens takes the
+ * new ones' scale alone.
  * Tokens whose number would be negative are skipped (their queries are rotated all the same).  No page that receives rows may belong to
  * two requests.  Bases and strides of pools, q, k_new, v_new and q_out in multiples of 16 bytes, and at most 2^24 - 1 rows (for fp8: rows of
  * queries and pages with new rows times KV heads), else PILLAR_EUNSUPPORTED. */

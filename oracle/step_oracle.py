@@ -99,7 +99,7 @@ def append_fp8(w, pool, scale, rows, starts):
                 if older > 0 and now != had:
                     ratio = f32(had / now)
                     pool[page, g, :older] = encode_e4m3((_TABLE[pool[page, g, :older]].astype(f32) * ratio).astype(f32))
-                inv = f32(f32(1) / now) if now > 0 else f32(0)
+                inv = f32(0) if now < f32(f32(2.0 ** -90) / f32(448)) else f32(f32(1) / now)
                 y = (x * inv).astype(f32)
                 y = np.where(np.abs(y) > 448, np.copysign(f32(448), y), y)
                 for i, (slot, _) in enumerate(new):

@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void append_pages(AppendArgs a, int pages
     for (int i = 0; i < kThreads / 64; ++i) most = fmaxf(most, s_max[w][i]);
     const float fresh = most < kLeastMax ? 0.f : most / 448.f;
     now[w] = older > 0 ? fmaxf(had[w], fresh) : fresh;
-    inv[w] = now[w] > 0.f ? 1.f / now[w] : 0.f;
+    inv[w] = now[w] < kLeastMax / 448.f ? 0.f : 1.f / now[w];            // (older tokens next to nothing: the new ones, which are no larger, are zeros)
   }
   if (tid == 0) {
     const_cast<float*>(kv.k_scale)[at_scale] = now[0];
