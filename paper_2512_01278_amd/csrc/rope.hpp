@@ -2,9 +2,9 @@
 //
 //   y1 = a (x1 cos t - x2 sin t),  y2 = a (x2 cos t + x1 sin t),  t = position * frequency of the pair
 //
-// A float cannot hold the angle of a far position (position 10^6 at frequency 1: the fraction of a turn to 2^-5), so it is worked out in turns in 64 bits, the
-// whole turns and then the quarters are taken off there, and what is left, at most an eighth of a turn either way, goes through the
-// power series of sine and cosine in fp32 (up to x^9 and x^10: within 2^-29 of either).
+// A float cannot hold the angle of a far position (position 10^6 at frequency 1: the fraction of a turn to 2^-5), and 64 bits hold that of the farthest to 2^-23
+// of a turn, so it is worked out in turns, in 64 bits and what their roundings leave.  The whole turns and then the quarters are taken off there,
+// and what is left, at most an eighth of a turn either way, goes through the power series of sine and cosine in fp32 (up to x^9 and x^10: within 2^-29 of either).
 #pragma once
 
 #include "common.hpp"
@@ -18,9 +18,11 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // cosine and sine of position * frequency, times amplitude
 __device__ __forceinline__ float2 turned(int position, double frequency, float amplitude) {
-  constexpr double kTurnsPerRadian = 0.15915494309189533577;
-  const double turns = static_cast<double>(position) * (frequency * kTurnsPerRadian);
-  const double part = turns - __builtin_rint(turns);                     // -1/2 .. 1/2
+  constexpr double kTurnsPerRadian = 0x1.45f306dc9c883p-3, kTurnsPerRadianLow = -0x1.6b01ec5417056p-57;        // 1 / 2 pi
+  const double p = static_cast<double>(position);
+  const double each = frequency * kTurnsPerRadian, each_low = __builtin_fma(frequency, kTurnsPerRadian, -each) + frequency * kTurnsPerRadianLow;
+  double part = __builtin_fma(p, each, -__builtin_rint(p * each)) + p * each_low;           // (the product is not rounded)
+  part -= __builtin_rint(part);                                          // -1/2 .. 1/2
   const double quarters = __builtin_rint(4.0 * part);                    // -2 .. 2
   const float x = static_cast<float>(__builtin_fma(quarters, -0.25, part)) * 6.28318530717958647692f;
   const int k = static_cast<int>(quarters);
