@@ -42,24 +42,38 @@ struct PromptSteps {
     const uint32_t k = n >> d;
     return (up_to(k) << d) + (n - (k << d)) * k;
   }
+  // the tiles ahead of the first that reads all of the cache: up to there, steps grow (there may be fewer tiles than that)
+  PILLAR_RULE int growing() const {
+    const int d = q_shift - t_shift;
+    if (d >= 0) {
+      const int a = static_cast<int>(from >> t_shift);
+      return cap > a ? (cap - a + (1 << d) - 1) >> d : 0;
+    }
+    const int room = static_cast<int>((static_cast<uint32_t>(cap) << -d) - (from >> q_shift));
+    return room < 0 ? 0 : room;
+  }
   // units of the tiles before r, r <= tiles
   PILLAR_RULE int before(int r) const {
-    const int d = q_shift - t_shift;
-    if (d >= 0) {                                        // steps(r) = a + (r << d) as long as that is below cap
-      const int a = static_cast<int>(from >> t_shift), room = cap > a ? (cap - a + (1 << d) - 1) >> d : 0, k = room < r ? room : r;
-      return static_cast<int>(static_cast<uint32_t>(k) * a + (up_to(k) << d) + static_cast<uint32_t>(r - k) * cap + static_cast<uint32_t>(r) * setup);
-    }
+    const int d = q_shift - t_shift, room = growing(), k = room < r ? room : r;
+    const uint32_t rest = static_cast<uint32_t>(r - k) * cap + static_cast<uint32_t>(r) * setup;
+    if (d >= 0) return static_cast<int>(static_cast<uint32_t>(k) * (from >> t_shift) + (up_to(k) << d) + rest);        // steps(r) = a + (r << d) as long as that is below cap
     const uint32_t a = from >> q_shift;
-    const int room = static_cast<int>((static_cast<uint32_t>(cap) << -d) - a), k = room < 0 ? 0 : room < r ? room : r;
-    return static_cast<int>(sum_of_shifted(a + k, -d) - sum_of_shifted(a, -d) + static_cast<uint32_t>(r - k) * cap + static_cast<uint32_t>(r) * setup);
+    return static_cast<int>(sum_of_shifted(a + k, -d) - sum_of_shifted(a, -d) + rest);
   }
   PILLAR_RULE int units() const { return tiles > 0 ? before(tiles) : 0; }
-  // the tile that has unit u, 0 <= u < units()
+  // The tile that has unit u, 0 <= u < units(), or one near it.  Of growing tiles, where steps grow by g = Q / T from tile to tile, those before r have
+  // s r + g r^2 / 2 units, s = steps(0) - g / 2 + setup, and this is its root.  With T > Q steps are stairs of T / Q tiles, (from + r Q) / T - 1/2 (1 - g) on the average, and the
+  // sum is off by T / 8 Q units at the most.  The other tiles are alike (with far more new rows than tokens in the cache, nearly all are).
+  PILLAR_RULE int tile_near(int u) const {
+    const int room = growing(), k = room < tiles ? room : tiles, grown = before(k);
+    if (u >= grown) return k + (u - grown) / (cap + setup);
+    const float g = static_cast<float>(1 << q_shift) / static_cast<float>(1 << t_shift);
+    const float s = setup + (q_shift >= t_shift ? static_cast<float>(from >> t_shift) - 0.5f * g : static_cast<float>(from >> q_shift) * g - 0.5f);
+    const int r = static_cast<int>(2.f * static_cast<float>(u) / (s + sqrt_of(s * s + 2.f * g * static_cast<float>(u))));
+    return r < 0 ? 0 : r >= k ? k - 1 : r;
+  }
   PILLAR_RULE int tile_of(int u) const {
-    // steps grow by Q / T from tile to tile, so the units before tile r are about (s - 1/2 step) r + Q / T r^2 / 2: its root, and then the few tiles it is off by
-    const float grow = static_cast<float>(1 << q_shift) / static_cast<float>(1 << t_shift), s = static_cast<float>(steps(0) + setup) - 0.5f * grow;
-    int r = static_cast<int>(2.f * static_cast<float>(u) / (s + sqrt_of(s * s + 2.f * grow * static_cast<float>(u))));
-    r = r < 0 ? 0 : r >= tiles ? tiles - 1 : r;
+    int r = tile_near(u);
     while (r > 0 && before(r) > u) --r;
     while (r + 1 < tiles && before(r + 1) <= u) ++r;
     return r;

@@ -1,7 +1,11 @@
 """What the calls around new tokens ask for and refuse, on the CPU."""
+import shutil
+import subprocess
+
 import pytest
 
 from paper_2512_01278_amd import binding as pb
+from tests.test_host_rules import CSRC
 
 
 @pytest.fixture(scope="module")
@@ -22,3 +26,52 @@ def test_a_workspace_of_log_probabilities_does_for_smaller_calls(lib):
             sizes = [need(r, vocab, top) for vocab in vocabs]
             assert sizes == sorted(sizes), (r, top)
     assert need((1 << 24) - 1, 1 << 30, 64) < 1 << 20                  # rows of one part leave nothing there
+
+
+MAIN = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "prompt_rules.hpp"
+// the tile of a unit by halving
+static int search(const pillar::PromptSteps& p, int u) {
+  int lo = 0, hi = p.tiles;
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (p.before(mid) <= u) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+int main(int, char** v) {
+  const pillar::PromptSteps p(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]));
+  const int units = p.units();
+  int furthest = 0;
+  for (int i = 0; i <= 4000; ++i) {
+    const int u = i < 1000 ? i : i < 2000 ? units - 1 - (i - 1000) : (int)((long long)(units - 1) * (i - 2000) / 2000);
+    if (u < 0 || u >= units) continue;
+    const int off = abs(p.tile_near(u) - search(p, u));
+    if (off > furthest) furthest = off;
+  }
+  printf("%d %d %d\n", p.tiles, units, furthest);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def near(tmp_path_factory):
+    d = tmp_path_factory.mktemp("tile_near")
+    (d / "main.cpp").write_text(MAIN)
+    subprocess.run([shutil.which("g++") or "c++", "-O1", "-std=c++17", "-I", CSRC, str(d / "main.cpp"), "-o", str(d / "near")], check=True)
+    return lambda *args: tuple(map(int, subprocess.run([str(d / "near"), *map(str, args)], check=True, capture_output=True, text=True).stdout.split()))
+
+
+@pytest.mark.parametrize("q_shift,t_shift,setup", [(0, 7, 1), (1, 7, 1), (3, 7, 1), (0, 6, 1), (4, 6, 4), (5, 6, 4), (6, 6, 4), (7, 6, 4), (8, 6, 4), (6, 6, 0)])
+@pytest.mark.parametrize("length,n", [(64, 1 << 20), (1, 1 << 20), (5000, 1 << 20), (1 << 20, 1 << 20), (1 << 20, 70000), (1 << 24, 1000), (300, 299), (100, 5000), (8192, 8192), (40000, 65536)])
+def test_a_units_tile_is_found_in_a_few_steps(near, length, n, q_shift, t_shift, setup):
+    """However many tiles there are, among them far more rows than tokens in the cache.  Where steps are stairs of T / Q tiles, the sum of what they are off their mean
+    is at most a quarter of a stair's width by half its height, T / 8 Q units, and a tile has a step at the least; the root and its rounding are off by two."""
+    if -(-n // (1 << q_shift)) * (-(-length // (1 << t_shift)) + setup) >= 1 << 30:
+        pytest.skip("more units than a call may have")
+    tiles, units, furthest = near(length, n, q_shift, t_shift, setup)
+    assert tiles == -(-n // (1 << q_shift)) and 0 < units < 1 << 30
+    assert furthest <= 2 + (1 << max(t_shift - q_shift, 0)) // 8, (tiles, units, furthest)
