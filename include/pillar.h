@@ -428,7 +428,8 @@ int pillar_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, do
  *   x    device [tokens][num_heads][head_dim] of `dtype` (PILLAR_F32 | PILLAR_BF16), token t at element t * x_stride (x_stride >= num_heads *
  *        head_dim: rows of a fused projection will do), heads dense within; out likewise.
  *   positions  device [tokens] int32.
- * out may be x itself with the same stride; else the two spans must not overlap (PILLAR_EINVAL).  head_dim 2..512, even; at most 2^24 - 1 tokens. */
+ * out may be x itself with the same stride; else the two spans must not overlap, nor may out's hold positions or frequencies, which the other tokens' workgroups
+ * still read (PILLAR_EINVAL).  head_dim 2..512, even; at most 2^24 - 1 tokens. */
 int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_heads, int32_t head_dim, int32_t dtype,
                   const int32_t* positions, const pillar_rope_t* rope, void* out, int64_t out_stride, void* hip_stream);
 

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -137,6 +138,15 @@ bool fits_a_grid(const pillar_kv_t* kv) { return kv->batch <= 65535 && kv->num_k
 
 // bytes from the first to past the last element of strided rows
 uint64_t span_of(int64_t rows, int64_t stride, int64_t row, int esz) { return static_cast<uint64_t>((rows - 1) * stride + row) * esz; }
+
+// what some workgroups of a launch read while others write their results
+struct Span {
+  const void* at;
+  uint64_t bytes;
+};
+bool over_any(const Span& result, std::initializer_list<Span> read) {
+  return std::any_of(read.begin(), read.end(), [&](const Span& r) { return result.at && r.at && overlap(result.at, result.bytes, r.at, r.bytes); });
+}
 
 // packed rows of new tokens
 int check_rows(const pillar_kv_t* kv, const int32_t* starts, int total_rows, int max_new) {
@@ -657,7 +667,9 @@ int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_h
   if (tokens == 0) return PILLAR_OK;
   const int esz = dtype == PILLAR_F32 ? 4 : 2;
   const bool in_place = x == out && x_stride == out_stride;
-  if (!in_place && overlap(x, span_of(tokens, x_stride, row, esz), out, span_of(tokens, out_stride, row, esz))) return PILLAR_EINVAL;
+  const Span result{out, span_of(tokens, out_stride, row, esz)};
+  if (!in_place && over_any(result, {{x, span_of(tokens, x_stride, row, esz)}})) return PILLAR_EINVAL;
+  if (over_any(result, {{positions, 4ull * tokens}, {rope->frequencies, 4ull * rope->rotary_dim}})) return PILLAR_EINVAL;
   a.x = x;
   a.out = out;
   a.x_stride = x_stride;

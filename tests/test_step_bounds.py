@@ -1,4 +1,5 @@
 """What the calls around new tokens ask for and refuse, on the CPU."""
+import ctypes as C
 import shutil
 import subprocess
 
@@ -75,3 +76,24 @@ def test_a_units_tile_is_found_in_a_few_steps(near, length, n, q_shift, t_shift,
     tiles, units, furthest = near(length, n, q_shift, t_shift, setup)
     assert tiles == -(-n // (1 << q_shift)) and 0 < units < 1 << 30
     assert furthest <= 2 + (1 << max(t_shift - q_shift, 0)) // 8, (tiles, units, furthest)
+
+
+# ------------------------------------------------------------ results over what is read ----
+FAR = [i << 40 for i in range(1, 20)]                      # addresses that overlap with nothing
+
+
+def around(at, bytes_, size):
+    """Addresses of a result of `size` bytes that lies over what is there, at its first and its last bytes."""
+    return at, at + bytes_ - 4, at - size + 4
+
+
+def test_rotated_rows_over_positions_or_frequencies_are_refused(lib):
+    tokens, heads, D = 1000, 4, 128
+    size = 2 * tokens * heads * D
+    x, positions, frequencies = FAR[:3]
+    call = lambda out, stride=heads * D, x=x: lib.pillar_rotate(x, heads * D, tokens, heads, D, pb.PILLAR_BF16, positions,
+                                                               C.byref(pb.pillar_rope_t(D, 0, 1.0, 0, frequencies)), out, stride, None)
+    for at, bytes_ in ((positions, 4 * tokens), (frequencies, 4 * D)):
+        for out in around(at, bytes_, size):
+            assert call(out) == pb.PILLAR_EINVAL, (at, out)
+            assert call(out, x=out) == pb.PILLAR_EINVAL, (at, out)         # (in place too)
