@@ -441,7 +441,8 @@ int pillar_rotate(const void* x, int64_t x_stride, int32_t tokens, int32_t num_h
  *   positions   device [total_rows] int32 for the rotation, or NULL: the number of the token in the cache, seq_lens[b] - n + i.  (After an
  *               eviction, and for the nodes of a tree, that is not the place in the text.)
  *   q, q_out    [total_rows][Hq][D] q_dtype, q_out dense, row t of q at element t * q_stride; both NULL: no queries.  q_out may be q itself
- *               if that is dense too, and must not overlap q, k_new or v_new otherwise (PILLAR_EINVAL).
+ *               if that is dense too, and must not overlap q, k_new or v_new otherwise, nor starts, positions, frequencies, or seq_lens, block_table
+ *               and scales of the cache (PILLAR_EINVAL).
  *   k_new, v_new  [total_rows][Hkv][D] q_dtype, row t at element t * k_stride, v_stride.
  * The cache may have any of its types: values are rounded once, to nearest even, from the fp32 result.  WRITES into the pools and, for fp8,
  * into k_scale and v_scale: a page gets the largest scale of its older tokens' (those before the new ones; their codes are rounded anew where it

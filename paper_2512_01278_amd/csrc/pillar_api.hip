@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
@@ -144,9 +145,19 @@ struct Span {
   const void* at;
   uint64_t bytes;
 };
-bool over_any(const Span& result, std::initializer_list<Span> read) {
+template <typename Spans>
+bool any_under(const Span& result, const Spans& read) {
   return std::any_of(read.begin(), read.end(), [&](const Span& r) { return result.at && r.at && overlap(result.at, result.bytes, r.at, r.bytes); });
 }
+bool over_any(const Span& result, std::initializer_list<Span> read) { return any_under(result, read); }
+// what says where the rows of a cache are, and their scales
+std::array<Span, 4> described_by(const pillar_kv_t* kv) {
+  const uint64_t scales = 4ull * kv->num_pages * kv->num_kv_heads;
+  const bool scaled = kv->kv_dtype == PILLAR_FP8_E4M3;
+  return {{{kv->seq_lens, 4ull * kv->batch}, {kv->block_table, 4ull * ((kv->batch - 1ull) * kv->block_table_stride + (kv->max_seq_len - 1ull) / kv->page_size + 1)},
+           {scaled ? kv->k_scale : nullptr, scales}, {scaled ? kv->v_scale : nullptr, scales}}};
+}
+bool over_any(const Span& result, const std::array<Span, 4>& read) { return any_under(result, read); }
 
 // packed rows of new tokens
 int check_rows(const pillar_kv_t* kv, const int32_t* starts, int total_rows, int max_new) {
@@ -701,11 +712,12 @@ int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, cons
   if (total_rows == 0) return PILLAR_OK;
   const int esz = kv->q_dtype == PILLAR_F32 ? 4 : 2;
   if (q) {
-    const uint64_t out_span = span_of(total_rows, q_row, q_row, esz);
+    const Span result{q_out, span_of(total_rows, q_row, q_row, esz)};
     const bool in_place = q == q_out && q_stride == q_row;
-    if ((!in_place && overlap(q, span_of(total_rows, q_stride, q_row, esz), q_out, out_span)) ||
-        overlap(k_new, span_of(total_rows, k_stride, kv_row, esz), q_out, out_span) ||
-        overlap(v_new, span_of(total_rows, v_stride, kv_row, esz), q_out, out_span))
+    if ((!in_place && over_any(result, {{q, span_of(total_rows, q_stride, q_row, esz)}})) || over_any(result, described_by(kv)) ||
+        over_any(result, {{k_new, span_of(total_rows, k_stride, kv_row, esz)}, {v_new, span_of(total_rows, v_stride, kv_row, esz)},
+                          {starts, 4ull * (kv->batch + 1)}, {positions, 4ull * total_rows},
+                          {rope ? rope->frequencies : nullptr, rope ? 4ull * rope->rotary_dim : 0}}))
       return PILLAR_EINVAL;
   }
   a.kv = make_view(kv);

@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2512_01278_amd import binding as pb
+from tests.test_abi import good_kv
 from tests.test_host_rules import CSRC
 
 
@@ -82,9 +83,9 @@ def test_a_units_tile_is_found_in_a_few_steps(near, length, n, q_shift, t_shift,
 FAR = [i << 40 for i in range(1, 20)]                      # addresses that overlap with nothing
 
 
-def around(at, bytes_, size):
-    """Addresses of a result of `size` bytes that lies over what is there, at its first and its last bytes."""
-    return at, at + bytes_ - 4, at - size + 4
+def around(at, bytes_, size, step=4):
+    """Addresses, in multiples of `step`, of a result of `size` bytes that lies over what is there, at its first and its last bytes."""
+    return at, at + (bytes_ - 1) // step * step, at - size + step
 
 
 def test_rotated_rows_over_positions_or_frequencies_are_refused(lib):
@@ -97,3 +98,31 @@ def test_rotated_rows_over_positions_or_frequencies_are_refused(lib):
         for out in around(at, bytes_, size):
             assert call(out) == pb.PILLAR_EINVAL, (at, out)
             assert call(out, x=out) == pb.PILLAR_EINVAL, (at, out)         # (in place too)
+
+
+def far_kv(**kw):
+    """A cache whose arrays lie far apart."""
+    more = dict(k_pool=FAR[10], v_pool=FAR[11], block_table=FAR[12], seq_lens=FAR[13])
+    if kw.get("kv_dtype") == pb.PILLAR_FP8_E4M3:
+        more.update(k_scale=FAR[14], v_scale=FAR[15])
+    return good_kv(**more, **kw)
+
+
+def described(kv):
+    """Arrays of the cache that every workgroup reads, and their bytes."""
+    spans = [(kv.seq_lens, 4 * kv.batch), (kv.block_table, 4 * ((kv.batch - 1) * kv.block_table_stride + kv.max_seq_len // kv.page_size))]
+    return spans + [(at, 4 * kv.num_pages * kv.num_kv_heads) for at in (kv.k_scale, kv.v_scale) if at]
+
+
+@pytest.mark.parametrize("kv_dtype", [pb.PILLAR_BF16, pb.PILLAR_FP8_E4M3])
+def test_rotated_queries_over_what_an_append_reads_are_refused(lib, kv_dtype):
+    kv, T = far_kv(kv_dtype=kv_dtype), 400
+    size = 2 * T * 32 * 128
+    starts, positions, frequencies, q, k, v = FAR[:6]
+
+    def call(q_out, rope=True, positions=positions):
+        r = C.byref(pb.pillar_rope_t(128, 0, 1.0, 0, frequencies)) if rope else None
+        return lib.pillar_append_rotated(C.byref(kv), r, starts, T, 100, positions, q, 4096, q_out, k, 1024, v, 1024, None)
+    for at, bytes_ in [(starts, 4 * 5), (positions, 4 * T), (frequencies, 4 * 128)] + described(kv):
+        for out in around(at, bytes_, size, 16):
+            assert call(out) == pb.PILLAR_EINVAL, (at, out)
