@@ -461,7 +461,8 @@ int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, cons
  *
  * Causal attention of any number of new tokens per request over its whole context: prompts, chunks of them, and single tokens beside
  * them.  Rows are packed as in pillar_append_rotated, whose tokens they are: row i of request b's n attends to tokens 0 .. seq_lens[b]-n+i.
- *   q, out  [total_rows][Hq][D] q_dtype, dense; no part of out or lse may be q (PILLAR_EINVAL).
+ *   q, out  [total_rows][Hq][D] q_dtype, dense; no part of out or lse may be q, starts, seq_lens, block_table or scales of the cache, nor the
+ *           other one of the two (PILLAR_EINVAL).
  *   lse     [total_rows][Hq] fp32 natural-log-sum-exp of the logits, or NULL.
  * A row that sees no token (its number is negative, or the request has no token) gets out = 0 and lse = -inf.  What a row does not see has no
  * influence on it, whatever the cache holds there.  Every shape that pillar_kv_t can describe, group sizes up to 16.  bf16 queries with a bf16

@@ -763,7 +763,10 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
   if (total_rows == 0) return PILLAR_OK;
   // several workgroups read a row of q, and one of them writes its result
   const uint64_t bytes = static_cast<uint64_t>(total_rows) * kv->num_q_heads * kv->head_dim * (kv->q_dtype == PILLAR_F32 ? 4 : 2);
-  if (overlap(q, bytes, out, bytes) || (lse && overlap(q, bytes, lse, 4ull * total_rows * kv->num_q_heads))) return PILLAR_EINVAL;
+  const Span rows{out, bytes}, sums{lse, 4ull * total_rows * kv->num_q_heads};
+  for (const Span& result : {rows, sums})
+    if (over_any(result, {{q, bytes}, {starts, 4ull * (kv->batch + 1)}}) || over_any(result, described_by(kv))) return PILLAR_EINVAL;
+  if (over_any(sums, {rows})) return PILLAR_EINVAL;
   a.q = q;
   a.starts = starts;
   a.total_rows = total_rows;

@@ -126,3 +126,18 @@ def test_rotated_queries_over_what_an_append_reads_are_refused(lib, kv_dtype):
     for at, bytes_ in [(starts, 4 * 5), (positions, 4 * T), (frequencies, 4 * 128)] + described(kv):
         for out in around(at, bytes_, size, 16):
             assert call(out) == pb.PILLAR_EINVAL, (at, out)
+
+
+@pytest.mark.parametrize("kv_dtype", [pb.PILLAR_BF16, pb.PILLAR_FP8_E4M3])
+def test_attention_of_new_tokens_over_what_it_reads_is_refused(lib, kv_dtype):
+    kv, T = far_kv(kv_dtype=kv_dtype), 400
+    size = {"out": 2 * T * 32 * 128, "lse": 4 * T * 32}
+    q, starts, free, other, ws = FAR[:5]
+    call = lambda out, lse: lib.pillar_prompt_attn(C.byref(kv), q, starts, T, 100, out, lse, ws, 1 << 39, None)
+    for at, bytes_ in [(q, size["out"]), (starts, 4 * 5)] + described(kv):
+        for out in around(at, bytes_, size["out"]):
+            assert call(out, None) == pb.PILLAR_EINVAL and call(out, other) == pb.PILLAR_EINVAL, (at, out)
+        for lse in around(at, bytes_, size["lse"]):
+            assert call(free, lse) == pb.PILLAR_EINVAL, (at, lse)
+    for lse in around(free, size["out"], size["lse"]):
+        assert call(free, lse) == pb.PILLAR_EINVAL, lse
