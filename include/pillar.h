@@ -492,7 +492,7 @@ int pillar_prompt_attn(const pillar_kv_t* kv, const void* q, const int32_t* star
  * them, are; +inf gives lse = +inf, -inf for finite tokens and NaN for itself.  Sums are fp32, of shares relative to one of the largest logits, whose own share is
  * kept apart: the log probability of a nearly certain token, and the entropy beside it, are exact to 10^-5 of themselves
  * (at the worst 2^-24 more for every 2048 logits beyond ten thousand).
- * No output may overlap logits or tokens, which others of a row's threads still read (PILLAR_EINVAL).
+ * No output may overlap logits or tokens, which others of a row's threads still read, or another output (PILLAR_EINVAL).
  * At most 2^24 - 1 rows, 2^30 logits and 2^30 given tokens in each (PILLAR_EUNSUPPORTED).
  * workspace: pillar_logprobs_workspace_bytes() (0: invalid arguments), enough for fewer rows, smaller vocabularies and fewer alternatives too. */
 size_t pillar_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);

@@ -802,9 +802,12 @@ int pillar_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32
   if (rc != PILLAR_OK) return rc;
   // a row's threads look at its logits and tokens until its last result is written
   const uint64_t read = span_of(rows, row_stride, vocab, static_cast<int>(esz)), asked = 4ull * rows * num_tokens, listed = 4ull * rows * top;
-  const std::pair<const void*, uint64_t> outs[] = {{logprobs, asked}, {lse, 4ull * rows}, {entropy, 4ull * rows}, {top_ids, listed}, {top_logprobs, listed}};
-  for (const auto& o : outs)
-    if (o.first && (overlap(logits, read, o.first, o.second) || (tokens && overlap(tokens, asked, o.first, o.second)))) return PILLAR_EINVAL;
+  const Span results[] = {{logprobs, asked}, {lse, 4ull * rows}, {entropy, 4ull * rows}, {top_ids, listed}, {top_logprobs, listed}};
+  for (int i = 0; i < 5; ++i) {
+    if (over_any(results[i], {{logits, read}, {tokens, asked}})) return PILLAR_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (over_any(results[i], {results[j]})) return PILLAR_EINVAL;
+  }
   LogprobArgs a;
   a.logits = logits;
   a.dtype = dtype;

@@ -141,3 +141,14 @@ def test_attention_of_new_tokens_over_what_it_reads_is_refused(lib, kv_dtype):
             assert call(free, lse) == pb.PILLAR_EINVAL, (at, lse)
     for lse in around(free, size["out"], size["lse"]):
         assert call(free, lse) == pb.PILLAR_EINVAL, lse
+
+
+def test_log_probabilities_over_each_other_are_refused(lib):
+    rows, vocab, m, top = 3, 1000, 5, 4
+    size = [4 * rows * n for n in (m, 1, 1, top, top)]
+    x, tok, ws = FAR[:3]
+    for i in range(5):
+        for j in range(5):
+            for bad in around(FAR[5 + j], size[j], size[i]) if i != j else ():
+                o = [bad if k == i else FAR[5 + k] for k in range(5)]
+                assert lib.pillar_token_logprobs(x, pb.PILLAR_BF16, rows, vocab, vocab, 1.0, tok, m, *o[:3], top, *o[3:], ws, 1 << 30, None) == pb.PILLAR_EINVAL, (i, j, bad)
