@@ -467,8 +467,8 @@ int pillar_append_rotated(const pillar_kv_t* kv, const pillar_rope_t* rope, cons
  * A row that sees no token (its number is negative, or the request has no token) gets out = 0 and lse = -inf.  What a row does not see has no
  * influence on it, whatever the cache holds there.  Every shape that pillar_kv_t can describe, group sizes up to 16.  bf16 queries with a bf16
  * or fp8 cache run on bf16 matrix instructions (P is rounded to bf16), if q, out, the pools and their strides are multiples of 16 bytes;
- * everything else, and with PILLAR_FLAG_GENERIC_KERNELS everything, on fp32 ones.  fp8 scales of what is seen are finite and not negative, and
- * a v_scale below 2^-80 counts as in pillar_verify_tree.  PILLAR_FLAG_EXACT_SCORES changes nothing here.  (A few tokens per request that
+ * everything else, and with PILLAR_FLAG_GENERIC_KERNELS everything, on fp32 ones.  fp8 scales of what is seen are not negative, 448 times each
+ * is finite, and a v_scale below 2^-80 counts as in pillar_verify_tree.  PILLAR_FLAG_EXACT_SCORES changes nothing here.  (A few tokens per request that
  * also want the statistic: pillar_verify_attn; trees: pillar_verify_tree.)
  * workspace: pillar_prompt_workspace_bytes() (0: invalid arguments), enough for any smaller batch, total_rows, max_new and max_seq_len too. */
 size_t pillar_prompt_workspace_bytes(const pillar_kv_t* kv, int32_t total_rows, int32_t max_new);

@@ -8,14 +8,14 @@
 // The 1 of m is never added to the rest.  Of a token that is nearly certain, 1 + R would keep what of R lies above 2^-24, while log(1 + R) and the entropy are
 // hardly more than R: 10^-4 of themselves off at 1 - p = 10^-3.  Apart from it they are exact to 10^-5 of themselves, however small.
 //
-//   logprob_pass   a workgroup per (row, part of the row): (M, S, A) and the `top` largest of the part
+//   logprob_pass   a workgroup per (row, part of the row): (m, R, A) and the `top` largest of the part
 //   logprob_join   a workgroup per row: joins the parts, looks the given tokens up
 //
 // The largest logits are kept by each wavefront as one sorted list over its 64 lanes.  A logit gets in when it comes before the list's last, which after
 // a few batches is rare; the maximum of a lane's batch, needed for m anyway, says whether to look.
 //
-// What bounds it: the rows at 4.4 TB/s (640 rows of 150000 bf16 logits: 44 us without alternatives; the same without the exponentials 39), and what the lists
-// cost, 5 us with one alternative, 15 with eight.  Branches by what a wavefront is have to be scalar ones (readfirstlane): as lanes of a mask, the loop waited for
+// What bounds it: the rows at 4.8 TB/s (640 rows of 150000 bf16 logits: 40 us without alternatives, read alone 28), with two or three rows to a compute unit, and what
+// the lists cost, 7 us with one alternative, 19 with eight.  Branches by what a wavefront is have to be scalar ones (readfirstlane): as lanes of a mask, the loop waited for
 // every load before its next turn.  A key is one whole number, because comparisons of two parts became branches, at every step of a sort.
 // More wavefronts to a row, or more parts, make more lists to fill (512 threads 52 us with one alternative, 256 49; 240 rows of 50001 fp32 with twenty 32 and
 // 28), deeper prefetch gains nothing (three batches 48.4, four 48.7).
@@ -31,16 +31,16 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 // No logit is further (log2) above the reference m than this.  A first token of more than p = 4/5 is the reference, then; with less, R is 1/4 and more and
-// nothing is lost in 1 + R.  A move takes a wavefront as long as a batch does: with every new largest 640 rows of 150000 took 50.8 us, so 46.9.
+// nothing is lost in 1 + R.  A move takes a wavefront as long as a batch does: with every new largest 640 rows of 150000 took 50.8 us, so 46.5.  (Rows that rise from
+// their first logit to their last move in every second batch: 53 us without alternatives instead of 43.)
 constexpr float kRoom = 2.f;
-
 
 // Half of x - m, which itself may be more than fp32 holds (logits of either sign near the type's end, under a small scale); factors on it are doubled.
 __device__ __forceinline__ float half_apart(float x, float m) { return __builtin_fmaf(x, 0.5f, -0.5f * m); }
 
 struct Sums {
-  float m, s, a;               // largest logit (-inf: none so far), R (NaN: there was one), A
-  // The one with the smaller maximum comes over with its largest, whose share is 1.
+  float m, s, a;               // reference (-inf: none so far), R (NaN: there was one), A
+  // Those with the smaller reference come over with it, whose share is 1.
   __device__ __forceinline__ void add(Sums o, float c) {
     const bool mine = m >= o.m;
     const float top = mine ? m : o.m, low = mine ? o.m : m;
@@ -454,7 +454,7 @@ struct Plan {
   int parts, each;
 };
 // Two workgroups to a compute unit, in parts of 4096 bf16 or 2048 fp32 logits at the least: shorter parts are more lists to join, longer ones take longer.  One row of
-// 150000 bf16 logits with eight alternatives, parts of 2048 / 4096 / 8192 / 16384: 17.1 / 13.6 / 13.4 / 15.7 us, of 32000 11.6 / 10.9 / 12.2 / 14.6.
+// 150000 bf16 logits with eight alternatives, parts of 2048 / 4096 / 8192 / 16384: 16.4 / 13.5 / 13.5 / 15.2 us, of 32000 12.1 / 12.4 / 13.2 / 14.3.
 int64_t wanted_workgroups() { return 2 * static_cast<int64_t>(num_cus()); }
 Plan plan_of(int rows, int vocab, int dtype) {
   const int per = dtype == PILLAR_F32 ? 4 : 8, vectors = vocab / per;

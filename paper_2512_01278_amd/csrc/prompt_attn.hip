@@ -11,7 +11,8 @@
 //                 inside a tile it leaves a partial (m, l, O)
 //   prompt_merge  joins the partials
 //
-// Four prompts of 8 K tokens, 32 heads on 8: 2520 us, 871 TFLOP/s; two chunks of 2 K after 30 K 2220 us, 940 TFLOP/s, where a product of 8192^3 by the library runs at 1180.
+// Four prompts of 8 K tokens, 32 heads on 8: 2400 us, 916 TFLOP/s; two chunks of 2 K after 30 K 2190 us, 970 TFLOP/s, where a product of 8192^3 by the library runs at
+// 1320 (on another card 2500 us, 877 TFLOP/s, and 1180).
 // Between the two lies what it takes to begin and end a tile.  (Two groups of wavefronts half a step apart, one at the products while the other takes
 // exponentials, gain nothing: 800 against 830 TFLOP/s at the time.)
 #include <algorithm>

@@ -4,8 +4,9 @@
 //   append_rows    queries, keys and values of new tokens, into a bf16 or fp32 cache, a workgroup per row
 //   append_pages   the same into an fp8 cache, keys and values by (page, KV head), because a page's scale is that of all its rows
 //
-// Bound by memory where there is much to move: every element is read once and written once, 32768 tokens of 32 heads (537 MB) in 106 us, 25 K tokens of 32 + 2 x 8 heads
-// with keys and values into their pages (638 MB) in 132 us, both at the rate of a large copy (4.8 TB/s).  Turns are worked out once per row, into LDS, for all its heads.
+// Bound by memory where there is much to move: every element is read once and written once, 32768 tokens of 32 heads (537 MB) in 108 us, 25 K tokens of 32 + 2 x 8 heads
+// with keys and values into their pages (638 MB) in 132 us, 5.0 and 4.8 TB/s: nine tenths of what copies of as many bytes run at (98 and 119 us).  Turns are worked out
+// once per row, into LDS, for all its heads.
 // Where there is little, by the launch: one token 4.7 us, of which the chain starts, lengths, page id, rows is the most.
 #include <algorithm>
 #include <type_traits>
