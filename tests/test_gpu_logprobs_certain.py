@@ -149,3 +149,19 @@ def test_a_workspace_for_many_rows_does_for_fewer():
             assert ((lp - whole[:R]).abs() <= 200 * 2.0 ** -24 * whole[:R].abs().clamp(min=1.0)).all(), R
             assert torch.equal(ids[:, 0].long(), x[:R].float().argmax(dim=1)), R
     assert (ws[size:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,V", [(520, 9000), (3, 50000)])
+def test_a_first_token_that_is_not_far_ahead(dtype, R, V):
+    """Up to p = 4/5 a runner-up that comes earlier may stay the reference: the first token is then one of the others' sum, 1 + R up to 5, and log p, 0.22 and more, the
+    difference of its logarithm and of 1.39.  A flat rest moves the reference three times at the most: 8 + 6 + 12 + 9 additions and moves and an exponent's 6 u, of which
+    R / (1 + R) counts, over 0.22, and 14 u for the difference: 163 u, 0.98e-5."""
+    x = torch.full((R, V), float(np.log(0.01 / V)))
+    at = V // 2
+    runner = np.empty(R, dtype=int)
+    for r in range(R):
+        p = (0.51, 0.6, 0.7, 0.78, 0.8, 0.82, 0.9)[r % 7]
+        runner[r] = at + (-2048, -4096, -512, -1, 1, 512, 2048, 100, -100)[(r // 7) % 9]
+        x[r, at], x[r, runner[r]] = float(np.log(p)), float(np.log(0.99 - p))
+    check((x + 3.0).to(QT[dtype]), 1.0, tokens_of(R, V, at, runner, R), 2)
